@@ -9,6 +9,7 @@
 
 #include "layer.hpp"
 #include "layer_kernels.hpp"
+#include "staging.hpp"
 
 namespace guide {
 namespace {
@@ -130,39 +131,21 @@ __global__ __launch_bounds__(WAVES * 64) void stream_kernel(guide_product_spec s
 
 // -------------------------------------------------------------------------------------------------- more rows: LDS tiles
 
-// A staged operand has rows of 128 bytes, so that a load takes whole cache lines (rows of 64 bytes cost 7 % of a large product).
-constexpr int kRow = 128;
-
-// Place of 16-byte piece c of row r in it: sixteen rows' pieces of one c fall into sixteen different slots of the 256 bytes that
-// LDS serves at once.
-__device__ __forceinline__ int swizzled(int r, int c) { return c ^ ((r >> 1) & 7); }
-
-// ROWS rows from memory to LDS; a wave's instruction moves 1024 bytes, which it lays down in the lanes' order, so that the
-// swizzle is on the memory's side (it repeats with every other instruction).  The buffer ends with the operand's last row and
-// answers reads beyond it with zeros; so does an offset past any end, which the lanes whose piece is beyond the end of k take
-// (`left` bytes of the row are real).
+// ROWS rows from memory to LDS; what is beyond the operand's last row, and beyond the end of k, becomes zeros (`left` bytes of the row
+// are real).
 template <int ROWS, int WAVES>
-struct Loader {
-    static constexpr int kLoads = ROWS * kRow / 1024 / WAVES, kRowsPer = 1024 / kRow, kForms = 2;       // instructions of a wave, rows of one
+struct Loader : TilePlaces<ROWS, WAVES> {
+    using Places = TilePlaces<ROWS, WAVES>;
     __amdgpu_buffer_rsrc_t rsrc;
-    int off[kForms], piece[kForms], stride;
 
     __device__ __forceinline__ void init(const uint8_t *base, uint32_t rows, int64_t row_stride, int64_t row_bytes, int wave, int lane) {
-        const int64_t bytes = (int64_t)(min(rows, (uint32_t)ROWS) - 1) * row_stride + row_bytes;
-        rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (int)bytes, 0x00020000);
-        stride = (int)row_stride;
-#pragma unroll
-        for (int i = 0; i < kForms; ++i) {
-            const int r = (wave * kLoads + i) * kRowsPer + lane / (kRow / 16);
-            piece[i] = swizzled(r, lane % (kRow / 16)) * 16;
-            off[i] = r * stride + piece[i];
-        }
+        rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (int)Places::bytes(rows, row_stride, row_bytes), 0x00020000);
+        Places::init(row_stride, wave, lane);
     }
     // instruction i of the wave's kLoads
     __device__ __forceinline__ void load(int i, int at, int left, uint8_t *lds, int wave) const {
-        const int o = piece[i % kForms] >= left ? (int)0x80000000 : off[i % kForms];
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(lds + (wave * kLoads + i) * 1024), 16, o,
-                                                 at + i / kForms * kForms * kRowsPer * stride, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(lds + (wave * Places::kLoads + i) * 1024), 16,
+                                                 (int)Places::of_lane(i, left), (int)Places::of_wave(at, left), 0, 0);
     }
 };
 

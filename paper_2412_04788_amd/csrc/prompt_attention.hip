@@ -3,11 +3,12 @@
 
 #include "attention_shared.hpp"
 #include "layer_kernels.hpp"
+#include "staging.hpp"
 
 namespace guide {
 namespace {
 
-constexpr int kRowsPerWave = 32, kTileK = 64;
+constexpr int kRowsPerWave = 32;
 
 // The sequence and the tile in it that tile number `tile` of the packed queries is (sequences have ceil(n_q / ROWS)
 // tiles each); false when there are fewer tiles.  Every lane of a wave looks at one sequence at a time.
@@ -52,41 +53,26 @@ __device__ inline bool find_tile(const guide_prompt_spec &s, uint32_t tile, Plac
 
 // 64 rows of D elements on their way to LDS, in which a row's 16-byte pieces are permuted: an instruction of a wave lays down
 // 1024 bytes in the lanes' order, so that the permutation is on the memory's side.
-// KEYS: rows are read 16 or 32 at a time, one piece of each; else (values) four at a time, 32 bytes of each.
-template <int D, bool KEYS>
-__device__ __forceinline__ int piece_of(int r, int c) {
-    if constexpr (KEYS) return D == 128 ? c ^ (r % 16) : c ^ (r / 2 % 8);
-    else return c ^ (r % 4 * (D / 32));
-}
-
 template <int D, bool KEYS, int WAVES>
-struct Sender {
-    static constexpr int kRow = D * 2, kRowsPer = 1024 / kRow, kLoads = kTileK / kRowsPer / WAVES;
-    // From one instruction to the next, the pieces of keys change by an exclusive or with a constant (D = 128: row bits 2 and
-    // 3, D = 64: row bit 3), those of values not at all.
-    static constexpr int kFlip = !KEYS ? 0 : 64;
-    uint32_t row_off, piece;                                         // the lane's place in the wave's first instruction
+struct Sender : KeyPlaces<D, KEYS, WAVES> {
+    using Places = KeyPlaces<D, KEYS, WAVES>;
     const uint8_t *next;                                             // the tile that is sent next, and the rows from it on
     int64_t stride;                                                  // bytes
     int left;
 
     __device__ __forceinline__ void init(const void *first, int64_t row_stride, int rows, int wave, int lane) {
         stride = row_stride * 2;
-        next = (const uint8_t *)first + (int64_t)(wave * kLoads * kRowsPer) * stride;
-        left = rows - wave * kLoads * kRowsPer;
-        const int r = lane / (kRow / 16);
-        row_off = (uint32_t)r * (uint32_t)stride;
-        piece = piece_of<D, KEYS>(wave * kLoads * kRowsPer + r, lane % (kRow / 16)) * 16;
+        next = (const uint8_t *)first + (int64_t)(wave * Places::kRows) * stride;
+        left = rows - wave * Places::kRows;
+        Places::init(stride, wave, lane);
     }
     // The wave's rows of a tile.  The buffer ends with the sequence's last row and answers what lies beyond with zeros.
     __device__ __forceinline__ void send(uint8_t *lds, int wave) {
-        const int rows = min(left, kLoads * kRowsPer);
-        const uint32_t bytes = rows > 0 ? (uint32_t)(rows - 1) * (uint32_t)stride + kRow : 0;
-        const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)next, 0, (int)bytes, 0x00020000);
+        const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)next, 0, (int)Places::bytes(left, stride), 0x00020000);
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(lds + (wave * kLoads + i) * 1024), 16,
-                                                     (int)(row_off + (piece ^ (uint32_t)(i * kFlip))), i * kRowsPer * (int)stride, 0, 0);
+        for (int i = 0; i < Places::kLoads; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(lds + (wave * Places::kLoads + i) * 1024), 16,
+                                                     (int)Places::of_lane(i, stride), 0, 0, 0);
         next += kTileK * stride;
         left -= kTileK;
     }
