@@ -6,6 +6,9 @@
 
 namespace guide {
 
+// Threads of a launch: HIP takes fewer than 2^32 along a dimension, and what needs more goes in several launches.
+constexpr uint64_t kMostThreads = 1ull << 31;
+
 hipError_t launch_quantise(const guide_quantise_spec &s, hipStream_t stream);
 hipError_t launch_norm(const guide_norm_spec &s, hipStream_t stream);
 // scratch: kScratch bytes that work split over blocks (a product's k, a prompt's keys) keeps its parts in.

@@ -83,9 +83,19 @@ __global__ __launch_bounds__(LANES < kBlock ? kBlock : LANES) void norm_kernel(g
 
 template <int T, int BITS>
 hipError_t quantise_as(const guide_quantise_spec &s, hipStream_t stream) {
-    const uint32_t per_row = (s.cols + 31u) / 32u * 4u, n = per_row * s.rows;
-    quantise_kernel<T, BITS><<<(n + kBlock - 1) / kBlock, kBlock, 0, stream>>>(s, make_div32(per_row), n);
-    return hipGetLastError();
+    const uint32_t per_row = (s.cols + 31u) / 32u * 4u, most = (uint32_t)(kMostThreads / per_row);        // (per_row <= 2^28)
+    guide_quantise_spec part = s;
+    for (uint32_t at = 0; at < s.rows; at += part.rows) {
+        part.rows = s.rows - at < most ? s.rows - at : most;
+        part.x = (const typename Elem<T>::type *)s.x + (int64_t)at * s.x_stride;
+        part.codes = s.codes + (int64_t)at * s.codes_stride;
+        part.scales = s.scales + (int64_t)at * s.scales_stride;
+        const uint32_t n = per_row * part.rows;
+        quantise_kernel<T, BITS><<<(n + kBlock - 1) / kBlock, kBlock, 0, stream>>>(part, make_div32(per_row), n);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 template <int T, int BITS>

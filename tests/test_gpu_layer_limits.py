@@ -1,0 +1,45 @@
+"""The layer operators at sizes that one launch does not hold, and at the ends of their stated limits."""
+import math
+
+import pytest
+
+from tests import layer_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    from paper_2412_04788_amd import guide
+    return guide.Context(0)
+
+
+@pytest.fixture(autouse=True)
+def memory():
+    """Tens of gigabytes each: given back before the next."""
+    import torch
+    torch.cuda.empty_cache()
+    yield
+    torch.cuda.empty_cache()
+
+
+def _repeats(torch, got, pattern):
+    """Whether the rows of `got` are those of `pattern` over and over."""
+    step = (1 << 24) // len(pattern) * len(pattern)
+    want = pattern.repeat(step // len(pattern), 1)
+    return all(torch.equal(part, want[:len(part)]) for part in got.split(step))
+
+
+@pytest.mark.parametrize("rows,cols", [((1 << 30) - 1, 1), ((1 << 25) - 1, 1000)])
+def test_quantise_of_nearly_2_30_groups(ctx, rows, cols):
+    import torch
+    some = torch.randn(1009, cols, generator=torch.Generator("cuda").manual_seed(1), device="cuda").bfloat16()
+    x = torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda")
+    for part in x.split(1009 << 10):
+        part.copy_(some.repeat(1 << 10, 1)[:len(part)])
+    groups = -(-cols // 32)
+    codes = torch.full((rows, groups * 16), 0xAA, dtype=torch.uint8, device="cuda")
+    scales = torch.full((rows, groups), 0xAA, dtype=torch.uint8, device="cuda")
+    ctx.quantise(x, codes, scales, bits=4)
+    want_c, want_s = ref.quantise(some, 4)
+    assert _repeats(torch, codes, want_c) and _repeats(torch, scales, want_s)
