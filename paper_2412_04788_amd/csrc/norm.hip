@@ -98,18 +98,36 @@ hipError_t quantise_as(const guide_quantise_spec &s, hipStream_t stream) {
     return hipSuccess;
 }
 
+template <int T, int BITS, int LANES, int CHUNKS>
+hipError_t norm_with(const guide_norm_spec &s, hipStream_t stream) {
+    using E = typename Elem<T>::type;
+    constexpr uint32_t kThreads = LANES < kBlock ? kBlock : LANES, kRows = kThreads / LANES, kMost = kMostThreads / LANES;
+    guide_norm_spec part = s;
+    for (uint32_t at = 0; at < s.rows; at += part.rows) {
+        part.rows = s.rows - at < kMost ? s.rows - at : kMost;
+        part.x = (const E *)s.x + (int64_t)at * s.x_stride;
+        if (s.residual) part.residual = (const E *)s.residual + (int64_t)at * s.residual_stride;
+        if (s.total) part.total = (E *)s.total + (int64_t)at * s.total_stride;
+        part.codes = s.codes + (int64_t)at * s.codes_stride;
+        part.scales = s.scales + (int64_t)at * s.scales_stride;
+        norm_kernel<T, BITS, LANES, CHUNKS><<<(part.rows + kRows - 1) / kRows, kThreads, 0, stream>>>(part);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 template <int T, int BITS>
 hipError_t norm_as(const guide_norm_spec &s, hipStream_t stream) {
-    const uint32_t chunks = (s.d + 7u) / 8u, rows = s.rows;
+    const uint32_t chunks = (s.d + 7u) / 8u;
     // a wave per row up to 1024 elements, a block beyond: 32 elements a lane at most
-    if (chunks <= 64) norm_kernel<T, BITS, 64, 1><<<(rows + 3) / 4, 256, 0, stream>>>(s);
-    else if (chunks <= 128) norm_kernel<T, BITS, 64, 2><<<(rows + 3) / 4, 256, 0, stream>>>(s);
-    else if (chunks <= 256) norm_kernel<T, BITS, 256, 1><<<rows, 256, 0, stream>>>(s);
-    else if (chunks <= 512) norm_kernel<T, BITS, 256, 2><<<rows, 256, 0, stream>>>(s);
-    else if (chunks <= 1024) norm_kernel<T, BITS, 256, 4><<<rows, 256, 0, stream>>>(s);
-    else if (chunks <= 2048) norm_kernel<T, BITS, 1024, 2><<<rows, 1024, 0, stream>>>(s);
-    else norm_kernel<T, BITS, 1024, 4><<<rows, 1024, 0, stream>>>(s);
-    return hipGetLastError();
+    if (chunks <= 64) return norm_with<T, BITS, 64, 1>(s, stream);
+    if (chunks <= 128) return norm_with<T, BITS, 64, 2>(s, stream);
+    if (chunks <= 256) return norm_with<T, BITS, 256, 1>(s, stream);
+    if (chunks <= 512) return norm_with<T, BITS, 256, 2>(s, stream);
+    if (chunks <= 1024) return norm_with<T, BITS, 256, 4>(s, stream);
+    if (chunks <= 2048) return norm_with<T, BITS, 1024, 2>(s, stream);
+    return norm_with<T, BITS, 1024, 4>(s, stream);
 }
 
 }  // namespace

@@ -43,3 +43,22 @@ def test_quantise_of_nearly_2_30_groups(ctx, rows, cols):
     ctx.quantise(x, codes, scales, bits=4)
     want_c, want_s = ref.quantise(some, 4)
     assert _repeats(torch, codes, want_c) and _repeats(torch, scales, want_s)
+
+
+@pytest.mark.parametrize("rows,d", [((1 << 26) + 3, 1), ((1 << 24) + 5, 1025)])
+def test_norm_of_more_rows_than_a_launch_holds(ctx, rows, d):
+    """Rows of a wave each, and rows of a block each."""
+    import torch
+    few = 1009
+    gen = torch.Generator("cuda").manual_seed(d)
+    some, weight = torch.randn(few, d, generator=gen, device="cuda").half(), torch.randn(d, generator=gen, device="cuda").half()
+    x = torch.empty(rows, d, dtype=torch.float16, device="cuda")
+    for part in x.split(few << 10):
+        part.copy_(some.repeat(1 << 10, 1)[:len(part)])
+    groups = -(-d // 32)
+    new = lambda n: (torch.full((n, groups * 16), 0xAA, dtype=torch.uint8, device="cuda"), torch.full((n, groups), 0xAA, dtype=torch.uint8, device="cuda"))  # noqa: E731
+    want, (codes, scales) = new(few), new(rows)
+    ctx.rms_norm(x, weight, codes, scales, residual=x, total=x, bits=4)
+    ctx.rms_norm(2 * some, weight, *want, bits=4)
+    assert _repeats(torch, codes, want[0]) and _repeats(torch, scales, want[1])
+    assert _repeats(torch, x, 2 * some)
