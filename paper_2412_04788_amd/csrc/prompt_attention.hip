@@ -555,20 +555,36 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(guide_prompt_spec s, u
     __builtin_memcpy((E *)s.out + (int64_t)(p.q0 + row) * s.out_stride + (int64_t)head * s.out_head_stride + ch, e, 8);
 }
 
+// launch(tiles, blocks) for the blocks of all tiles times heads, the last tiles first, as many at a time as a launch holds:
+// find_work() counts from the `tiles` that are left.
+template <class Launch>
+hipError_t over_tiles(uint32_t tiles, uint32_t n_h, Launch launch) {
+    const uint32_t most = (uint32_t)(kMostThreads / 512 / n_h);      // (n_h < 2^16)
+    for (uint32_t left = tiles; left;) {
+        const uint32_t some = left < most ? left : most;
+        launch(left, some * n_h);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        left -= some;
+    }
+    return hipSuccess;
+}
+
 template <int T, int D>
 hipError_t prompt_as(const guide_prompt_spec &s, float *scratch, hipStream_t stream) {
     // The pairs of groups pay where their turns are many and their tiles of 256 queries fill the chip: 8192 queries over 32 768
     // keys 1182 against 1113 TFLOP/s, 4096 over 8192 1057 against 1004; equal at 2048 keys to a query, behind with fewer, with
     // fewer tiles than compute units (512 queries of 64 heads: 742 against 912) and with 64 channels (945 against 980).
+    const uint32_t filled = s.n_seq < s.total_q ? s.n_seq : s.total_q;              // sequences that can have queries
     const uint64_t keys = (2ull * s.total_k > s.total_q ? 2ull * s.total_k - s.total_q : 0) / (2 * s.n_seq);     // that a query sees, about
     if constexpr (D == 128) {
         if (keys >= 4096 && (uint64_t)(s.total_q / 256) * s.n_h >= kNumCU) {
-            const uint32_t tiles = s.total_q / 256 + s.n_seq;
-            prompt_pair_kernel<T, D><<<tiles * s.n_h, 512, 0, stream>>>(s, tiles);
-            return hipGetLastError();
+            return over_tiles(s.total_q / 256 + filled, s.n_h, [&](uint32_t left, uint32_t blocks) {
+                prompt_pair_kernel<T, D><<<blocks, 512, 0, stream>>>(s, left);
+            });
         }
     }
-    const uint32_t tiles = s.total_q / 128 + s.n_seq;                // at least as many as there are
+    const uint32_t tiles = s.total_q / 128 + filled;                // at least as many as there are
     // Too few tiles to give every compute unit two blocks: keys are split.  Whole / split, 32 heads on 8 of 128: 1 query over 8001 keys 135 /
     // 26 us, 256 over 32 256 536 / 155, 512 over 8512 154 / 97.  Of the least number of keys to a part, 256 / 512: 1 over 1001 15.9 / 23.5,
     // 64 over 1064 19.6 / 21.4; but with more rows to join, 128 over 2128 of 32 heads 29 / 26, 1500 over 1500 of 12 heads 37.7 / 32.2.
@@ -577,14 +593,17 @@ hipError_t prompt_as(const guide_prompt_spec &s, float *scratch, hipStream_t str
     uint64_t parts = 2 * kNumCU / fewest;
     for (const uint64_t most : {keys / ((uint64_t)s.total_q * s.n_h <= 2048 ? 256 : 512), room, (uint64_t)kMostParts}) parts = parts < most ? parts : most;
     if (parts < 2) {
-        prompt_kernel<T, D, false><<<tiles * s.n_h, 256, 0, stream>>>(s, tiles, nullptr);
-        return hipGetLastError();
+        return over_tiles(tiles, s.n_h, [&](uint32_t left, uint32_t blocks) {
+            prompt_kernel<T, D, false><<<blocks, 256, 0, stream>>>(s, left, nullptr);
+        });
     }
-    prompt_kernel<T, D, true><<<dim3(tiles * s.n_h, (uint32_t)parts), 256, 0, stream>>>(s, tiles, scratch);
-    const hipError_t e = hipGetLastError();
+    const hipError_t e = over_tiles(tiles, s.n_h, [&](uint32_t left, uint32_t blocks) {
+        prompt_kernel<T, D, true><<<dim3(blocks, (uint32_t)parts), 256, 0, stream>>>(s, left, scratch);
+    });
     if (e != hipSuccess) return e;
-    prompt_join_kernel<T, D><<<dim3(tiles * s.n_h, 128 * (D / 4) / 256), 256, 0, stream>>>(s, tiles, scratch, (uint32_t)parts);
-    return hipGetLastError();
+    return over_tiles(tiles, s.n_h, [&](uint32_t left, uint32_t blocks) {
+        prompt_join_kernel<T, D><<<dim3(blocks, 128 * (D / 4) / 256), 256, 0, stream>>>(s, left, scratch, (uint32_t)parts);
+    });
 }
 
 }  // namespace

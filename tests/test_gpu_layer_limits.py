@@ -62,3 +62,34 @@ def test_norm_of_more_rows_than_a_launch_holds(ctx, rows, d):
     ctx.rms_norm(2 * some, weight, *want, bits=4)
     assert _repeats(torch, codes, want[0]) and _repeats(torch, scales, want[1])
     assert _repeats(torch, x, 2 * some)
+
+
+def _starts(torch, counts):
+    return torch.cat((torch.zeros(1, dtype=torch.int64), torch.tensor(counts).cumsum(0))).int().cuda()
+
+
+@pytest.mark.parametrize("heads,kv", [(4096, 8), (4100, 1)])
+def test_prompts_of_more_blocks_than_a_launch_holds(ctx, heads, kv):
+    """4096 sequences of one token, thousands of heads: every head gives its token's value."""
+    import torch
+    n, d = 4096, 64
+    gen = torch.Generator("cuda").manual_seed(heads)
+    k, v = (torch.randn(n, kv, d, generator=gen, device="cuda").half() for _ in range(2))
+    q = torch.ones(1, heads, d, dtype=torch.float16, device="cuda").repeat(n, 1, 1)
+    out = torch.full_like(q, math.nan)
+    starts = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    ctx.prompt_attention(q, k, v, starts, starts, out)
+    assert torch.equal(out, v.repeat_interleave(heads // kv, 1))
+
+
+def test_prompts_most_of_which_are_empty(ctx):
+    """2^20 sequences of which 128 have a token (with 4096 heads, tiles times heads pass 2^32 if the empty ones count)."""
+    import torch
+    n, heads, d = 128, 4096, 64
+    gen = torch.Generator("cuda").manual_seed(3)
+    k, v = (torch.randn(n, 1, d, generator=gen, device="cuda").bfloat16() for _ in range(2))
+    q = torch.ones(n, heads, d, dtype=torch.bfloat16, device="cuda")
+    out = torch.full_like(q, math.nan)
+    starts = _starts(torch, [1] * n + [0] * ((1 << 20) - n))
+    ctx.prompt_attention(q, k, v, starts, starts, out)
+    assert torch.equal(out, v.expand(n, heads, d))
