@@ -389,9 +389,19 @@ __global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : kBlock) void cache_join_ke
 
 template <int T, int D, bool READ>
 hipError_t tokens_as(const guide_cache &c, const guide_cache_tokens &t, hipStream_t stream) {
-    constexpr uint32_t kTokens = kBlock / (D / 8);
-    cache_tokens_kernel<T, D, READ><<<dim3((t.tokens + kTokens - 1) / kTokens, c.n_kv), kBlock, 0, stream>>>(view_of(c), t);
-    return hipGetLastError();
+    using E = typename Elem<T>::type;
+    constexpr uint32_t kTokens = kBlock / (D / 8), kMost = kMostThreads / (D / 8);
+    guide_cache_tokens part = t;
+    for (uint32_t at = 0; at < t.tokens; at += part.tokens) {
+        part.tokens = t.tokens - at < kMost ? t.tokens - at : kMost;
+        part.k = (E *)t.k + (int64_t)at * t.k_stride;
+        part.v = (E *)t.v + (int64_t)at * t.v_stride;
+        part.slots = t.slots + at;
+        cache_tokens_kernel<T, D, READ><<<dim3((part.tokens + kTokens - 1) / kTokens, c.n_kv), kBlock, 0, stream>>>(view_of(c), part);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 template <bool READ>

@@ -93,3 +93,21 @@ def test_prompts_most_of_which_are_empty(ctx):
     starts = _starts(torch, [1] * n + [0] * ((1 << 20) - n))
     ctx.prompt_attention(q, k, v, starts, starts, out)
     assert torch.equal(out, v.expand(n, heads, d))
+
+
+def test_more_tokens_than_a_launch_holds(ctx):
+    """2^28 tokens to append and read back, all but the last 1000 of them outside the cache."""
+    import torch
+    n, d, block, few = (1 << 28) + 7, 128, 16, 1000
+    codes = torch.zeros(64, 1, 2, block, d // 2, dtype=torch.uint8, device="cuda")
+    scales = torch.zeros(64, 1, 2, d // 32, block, dtype=torch.uint8, device="cuda")
+    slots = torch.full((n,), -1, dtype=torch.int64, device="cuda")
+    slots[n - few:] = torch.randperm(64 * block, generator=torch.Generator("cuda").manual_seed(2), device="cuda")[:few]
+    x = torch.empty(n, 1, d, dtype=torch.bfloat16, device="cuda")                   # 69 GB: keys and values alike
+    x[n - few:] = torch.randn(few, 1, d, generator=torch.Generator("cuda").manual_seed(1), device="cuda").bfloat16()
+    held = ref.decode(*ref.quantise(x[n - few:, 0], 4), 4, d)
+    ctx.cache_append(x, x, slots, codes, scales)
+    x.fill_(7)
+    ctx.cache_read(slots, codes, scales, x, x)
+    assert torch.equal(x[n - few:, 0].double(), held)
+    assert not any(part.any() for part in x[:n - few].view(torch.int16).split(1 << 24))
