@@ -303,6 +303,13 @@ def _shaped(what: str, t, shape):
         raise ValueError(f"{what}: shape {tuple(t.shape)}, {tuple(shape)} is needed")
 
 
+def _counts(*n):
+    """Counts go to the library in 32 bits."""
+    for x in n:
+        if x >> 32:
+            raise ValueError(f"{x} rows or tokens: fewer than 2^32 are needed")
+
+
 def _codes(what: str, t, shape):
     """Pointer and row stride of a matrix of bytes."""
     _shaped(what, t, shape)
@@ -572,6 +579,7 @@ class Context:
         """Pointers and strides of code and scale buffers of `rows` rows of `cols` values."""
         if bits != 4 and bits != 8:
             raise ValueError(f"codes of {bits} bits: 4 or 8")
+        _counts(rows, cols)
         groups = -(-cols // MX_GROUP)
         return (*_codes("codes", codes, (rows, groups * 4 * bits)), *_codes("scales", scales, (rows, groups)))
 
@@ -614,6 +622,7 @@ class Context:
         """Causal attention of packed sequences: q, out [total_q, n_h, d], k, v [total_k, n_kv, d], starts int32 [n_seq + 1]."""
         shape, dtype = q.shape, q.dtype
         (tq, n_h, d), (tk, n_kv, dk), n = shape, k.shape, q_starts.numel()
+        _counts(tq, tk, n)
         _shaped("out", out, shape)
         _shaped("v", v, k.shape)
         _shaped("q_starts", q_starts, (n,))
@@ -637,6 +646,7 @@ class Context:
     def _cache_tokens(self, fn, k, v, slots, codes, scales, stream):
         cache = self._cache(codes, scales)
         shape = (slots.numel(), cache.n_kv, cache.d)
+        _counts(shape[0])
         _shaped("k", k, shape)
         _shaped("v", v, shape)
         (pk, ks), (pv, vs) = _strided(k, 3), _strided(v, 3, k.dtype)
@@ -659,6 +669,7 @@ class Context:
         cache = self._cache(codes, scales)
         shape = q.shape
         n_seq, n_h, d = shape
+        _counts(n_seq)
         if d != cache.d:
             raise ValueError(f"head dimensions {d} and {cache.d}")
         _shaped("out", out, shape)

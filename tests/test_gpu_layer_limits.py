@@ -111,3 +111,23 @@ def test_more_tokens_than_a_launch_holds(ctx):
     ctx.cache_read(slots, codes, scales, x, x)
     assert torch.equal(x[n - few:, 0].double(), held)
     assert not any(part.any() for part in x[:n - few].view(torch.int16).split(1 << 24))
+
+
+def test_counts_that_32_bits_do_not_hold(ctx):
+    """2^32 rows are not none (one row's memory stands for all of them)."""
+    import torch
+    n = 1 << 32
+    rows = lambda c, dt: torch.zeros(1, c, dtype=dt, device="cuda").expand(n, c)  # noqa: E731
+    x, w, codes, scales = rows(1, torch.bfloat16), torch.ones(1, dtype=torch.bfloat16, device="cuda"), rows(16, torch.uint8), rows(1, torch.uint8)
+    one = torch.zeros(1, 16, dtype=torch.uint8, device="cuda"), torch.zeros(1, 1, dtype=torch.uint8, device="cuda")
+    heads = torch.zeros(1, 1, 64, dtype=torch.bfloat16, device="cuda")
+    many, starts = heads.expand(n, 1, 64), torch.zeros(2, dtype=torch.int32, device="cuda")
+    cache = torch.zeros(1, 1, 2, 16, 32, dtype=torch.uint8, device="cuda"), torch.zeros(1, 1, 2, 2, 16, dtype=torch.uint8, device="cuda")
+    slots = torch.zeros(1, dtype=torch.int64, device="cuda").expand(n)
+    for call in (lambda: ctx.quantise(x, codes, scales, bits=4), lambda: ctx.rms_norm(x, w, codes, scales, bits=4),
+                 lambda: ctx.product(codes, scales, *one, x, bits=4), lambda: ctx.product(*one, codes, scales, x.t(), bits=4),
+                 lambda: ctx.prompt_attention(many, heads, heads, starts, starts, many), lambda: ctx.prompt_attention(heads, many, many, starts, starts, heads),
+                 lambda: ctx.cache_append(many, many, slots, *cache), lambda: ctx.cache_read(slots, *cache, many, many),
+                 lambda: ctx.cache_attention(many, *cache, starts[:1].expand(n, 1), starts[:1].expand(n), many)):
+        with pytest.raises(ValueError):
+            call()
