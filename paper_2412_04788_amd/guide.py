@@ -295,7 +295,14 @@ def _strided(t, dims: int, dtype=None):
         raise ValueError(f"a CUDA tensor of {dims} dimensions with a contiguous last one is needed")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"dtypes differ: {t.dtype} and {dtype}")
+    if dims > 1 and t.shape[0] == 1:                             # a stride of no meaning, which torch leaves as it comes
+        st = (_one_row(t), *st[1:])
     return t.data_ptr(), st
+
+
+def _one_row(t) -> int:
+    """A row stride that passes the library's checks, for a tensor of one row."""
+    return -(-t.shape[-1] // 16) * 16
 
 
 def _shaped(what: str, t, shape):

@@ -1,0 +1,46 @@
+"""How the layer operators are called: tensors of one row or token as torch leaves them, streams, captured calls."""
+import math
+
+import pytest
+
+from tests import layer_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    from paper_2412_04788_amd import guide
+    return guide.Context(0)
+
+
+def _buffers(torch, rows, cols, bits):
+    g = -(-cols // 32)
+    return (torch.full((rows, g * 4 * bits), 0xAA, dtype=torch.uint8, device="cuda"),
+            torch.full((rows, g), 0xAA, dtype=torch.uint8, device="cuda"))
+
+
+def test_one_row_that_was_a_column(ctx):
+    """A column that is turned round is contiguous to torch, whatever the stride of its only row says."""
+    import torch
+    gen = torch.Generator("cuda").manual_seed(0)
+    turned = lambda t: t.new_empty(t.shape[1], 1).copy_(t.t()).t().contiguous()  # noqa: E731
+    x, w = torch.randn(1, 96, generator=gen, device="cuda").half(), torch.ones(96, dtype=torch.float16, device="cuda")
+    wc, ws = ref.quantise(torch.randn(5, 96, generator=gen, device="cuda"), 4)
+    got = []
+    for form in (lambda t: t, turned):
+        a, b = _buffers(torch, 1, 96, 8), _buffers(torch, 1, 96, 4)
+        a, b, total, out = [form(t) for t in a], [form(t) for t in b], form(torch.zeros_like(x)), form(torch.zeros(1, 5, dtype=torch.float16, device="cuda"))
+        assert form is not turned or x.shape == form(x).shape and form(x).stride(0) == 1 and a[0].stride(0) == 1
+        ctx.rms_norm(form(x), w, *a, residual=form(x), total=total)
+        ctx.product(*a, wc, ws, out)
+        ctx.quantise(form(x), *b, bits=4)
+        got.append((*a, *b, total, out))
+    for one, other in zip(*got):
+        assert torch.equal(one, other)
+    # one sequence's pages
+    codes, scales = torch.full((3, 1, 2, 16, 32), 0x22, dtype=torch.uint8, device="cuda"), torch.full((3, 1, 2, 2, 16), 127, dtype=torch.uint8, device="cuda")
+    q, out = torch.ones(1, 1, 64, dtype=torch.float16, device="cuda"), torch.zeros(1, 1, 64, dtype=torch.float16, device="cuda")
+    pages = turned(torch.tensor([[2, 0, 1]], dtype=torch.int32, device="cuda"))
+    ctx.cache_attention(q, codes, scales, pages, torch.tensor([40], dtype=torch.int32, device="cuda"), out)
+    assert (out == 1).all()
