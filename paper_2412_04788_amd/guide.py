@@ -661,7 +661,8 @@ class Context:
         self._invoke(fn, self._h, cache, spec, _stream_ptr(stream))
 
     def cache_append(self, k, v, slots, codes, scales, stream=None):
-        """Writes k, v [tokens, n_kv, d] to the slots (int64, page * kv_block + offset) of the cache."""
+        """Writes k, v [tokens, n_kv, d] to the slots (int64, page * kv_block + offset) of the cache, each a slot of its own or one outside
+        the cache (-1), which is skipped."""
         self._cache_tokens(self._lib.guide_cache_append, k, v, slots, codes, scales, stream)
 
     def cache_read(self, slots, codes, scales, k, v, stream=None):

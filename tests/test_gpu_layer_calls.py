@@ -44,3 +44,30 @@ def test_one_row_that_was_a_column(ctx):
     pages = turned(torch.tensor([[2, 0, 1]], dtype=torch.int32, device="cuda"))
     ctx.cache_attention(q, codes, scales, pages, torch.tensor([40], dtype=torch.int32, device="cuda"), out)
     assert (out == 1).all()
+
+
+@pytest.mark.parametrize("tokens", [9, 700])
+def test_append_with_tokens_to_skip_and_tokens_that_share_a_slot(ctx, tokens):
+    """Tokens outside the cache are skipped; what shares a slot stays in that slot."""
+    import torch
+    kv, d, block, pages = 3, 64, 16, -(-tokens // 16) + 1
+    gen = torch.Generator("cuda").manual_seed(tokens)
+    k, v = (torch.randn(tokens, kv, d, generator=gen, device="cuda").bfloat16() for _ in range(2))
+    slots = torch.randperm(pages * block, generator=gen, device="cuda")[:tokens]
+    slots[::3] = -1
+    slots[tokens // 2] = pages * block
+    shared = int(slots[1])
+    slots[tokens - 1], k[tokens - 1] = shared, k[tokens - 1] * 1024
+    keep = (slots >= 0) & (slots < pages * block) & (slots != shared)
+    codes = torch.full((pages, kv, 2, block, d // 2), 0xAA, dtype=torch.uint8, device="cuda")
+    scales = torch.full((pages, kv, 2, d // 32, block), 0xFF, dtype=torch.uint8, device="cuda")
+    want = codes.clone(), scales.clone()
+    page, at = slots[keep] // block, slots[keep] % block
+    for which, x in enumerate((k[keep], v[keep])):
+        c, s = ref.quantise(x.reshape(-1, d), 4)
+        want[0][page, :, which, at], want[1][page, :, which, :, at] = c.view(-1, kv, d // 2), s.view(-1, kv, d // 32)
+    ctx.cache_append(k, v, slots, codes, scales)
+    for got, right in ((codes.transpose(3, 4), want[0].transpose(3, 4)), (scales, want[1])):
+        got[shared // block, ..., shared % block] = 0
+        right[shared // block, ..., shared % block] = 0
+        assert torch.equal(got, right)
