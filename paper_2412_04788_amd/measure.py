@@ -3,7 +3,7 @@
 The performance model prices a layer's tasks at a card's peak and bandwidth, which a sweep multiplies by efficiency samples
 (e_c, e_b).  This module runs those tasks -- norms, products with 4-bit weights, prompt attention, a paged 4-bit KV cache and
 the attention of single tokens over it -- at a shape of the user's, and compares the time of a prefill pass and of a decode
-pass with what guide_eval_grid says of the same layer: e_c is the ratio for the prefill pass (compute bound), e_b for the
+pass with the performance model's price of the same layer: e_c is the ratio for the prefill pass (compute bound), e_b for the
 decode pass (bandwidth bound).  The pairs go into Context.eval_grid(e_c=..., e_b=...).
 
     python -m paper_2412_04788_amd.measure --model dense-7b --prompts 700,300,1048 --batch 16 --context 4096
@@ -125,16 +125,25 @@ def _seconds(run, repeats: int):
     return np.array(times)
 
 
-def modelled(ctx: guide.Context, model: wl.Model, hw: wl.Hardware, batch: int, s_in: int, s_out: int, kv_block: int):
-    """(prefill, decode step) seconds of one layer of `model` at 4-bit weights, by guide_eval_grid."""
-    one = wl.Model("layer", 1, model.d, model.n_h, model.n_kv, model.d_ff, V=1)
-    ctx.set_models(wl.models_array([one]))
-    ctx.set_hardware(wl.hw_array([hw]))
-    axes = [[0], [0], [batch], [s_in], [s_out], [1], [4], [kv_block], [batch * s_in]]
-    grid = guide.GridArg([(a, 0) for a in axes])
-    out = {k: torch.empty(1, dtype=torch.float64, device="cuda") for k in ("t_prefill", "t_decode")}
-    ctx.eval_grid(grid, 0, 1, out=out)
-    return float(out["t_prefill"]), float(out["t_decode"]) / max(s_out - 1, 1)
+def roofline(model: wl.Model, hw: wl.Hardware, tokens: float, pairs: float, keys: float, weight_bytes: float = 0.5, kv_bytes: float = 2.0):
+    """Seconds of one dense layer's tasks on one GPU at the record's rates, as guide.h's performance model has them (roofline): a pass
+    over `tokens` tokens with `pairs` query-key pairs that reads `keys` cached tokens."""
+    d, d_h, t = model.d, model.d // model.n_h, tokens
+    dq, dkv, ff = model.n_h * d_h, model.n_kv * d_h, model.d_ff
+    w = lambda n: weight_bytes * n  # noqa: E731
+    tasks = ((2 * t * d * (dq + 2 * dkv), w(d * (dq + 2 * dkv)) + 2 * t * d + 2 * t * (dq + 2 * dkv)),      # qkv
+             (4 * dq * pairs, 4 * t * dq + 2 * kv_bytes * dkv * keys),                                       # attention
+             (2 * t * dq * d, w(dq * d) + 2 * t * dq + 2 * t * d),                                           # out-proj
+             (4 * t * d * ff, w(2 * d * ff) + 2 * t * d + 4 * t * ff),                                       # ffn-up
+             (2 * t * ff * d, w(ff * d) + 2 * t * ff + 2 * t * d),                                           # ffn-down
+             (0, 8 * t * d))                                                                                 # norms
+    return sum(max(f / hw.peak_flops, b / hw.hbm_bw) for f, b in tasks)
+
+
+def nominal(model: wl.Model, hw: wl.Hardware, prompts, batch: int, context: int):
+    """(prefill, decode) seconds of a layer at the record's rates: a pass over `prompts`, a step of `batch` tokens at `context`."""
+    n, s = len(prompts), max(1, round(sum(prompts) / len(prompts)))      # prompts of their mean length
+    return (roofline(model, hw, n * s, n * s * s, n * s), roofline(model, hw, batch, batch * context, batch * context))
 
 
 def efficiency_samples(ctx: guide.Context, model: wl.Model, hw: wl.Hardware, prompts, batch: int, context: int, kv_block: int = 32,
@@ -166,9 +175,7 @@ def efficiency_samples(ctx: guide.Context, model: wl.Model, hw: wl.Hardware, pro
     px, pr = rows(total), rows(total)
     t_prefill = _seconds(lambda: layer.prefill(px, pr, starts, slots), repeats)
 
-    # the model's prefill of prompts of different lengths: the pass of their mean length
-    m_prefill, _ = modelled(ctx, model, hw, len(prompts), max(1, round(total / len(prompts))), 2, kv_block)
-    _, m_decode = modelled(ctx, model, hw, batch, max(context - 1, 1), 2, kv_block)
+    m_prefill, m_decode = nominal(model, hw, prompts, batch, context)
     return dict(t_prefill=t_prefill, t_decode=t_decode, m_prefill=m_prefill, m_decode=m_decode, e_c=m_prefill / t_prefill,
                 e_b=m_decode / t_decode)
 

@@ -71,3 +71,23 @@ def test_append_with_tokens_to_skip_and_tokens_that_share_a_slot(ctx, tokens):
         got[shared // block, ..., shared % block] = 0
         right[shared // block, ..., shared % block] = 0
         assert torch.equal(got, right)
+
+
+def test_measuring_leaves_the_context_alone(ctx):
+    """The caller's models and hardware answer as before after a measurement on the same context."""
+    import torch
+    from paper_2412_04788_amd import guide, measure, workloads as wl
+    g = wl.grid_tiny()
+    ctx.set_models(wl.models_array(g.models))
+    ctx.set_hardware(wl.hw_array(g.hws))
+    grid = guide.GridArg([(a.values, a.geom2_start) for a in g.axes])
+
+    def answers():
+        out = {k: torch.zeros(g.size, dtype=torch.float64, device="cuda") for k in ("t_prefill", "t_decode")}
+        ctx.eval_grid(grid, 0, g.size, out=out)
+        return out
+    before = answers()
+    small = wl.Model("small", 1, 256, 4, 2, 448, V=32)
+    measure.efficiency_samples(ctx, small, wl.Hardware(1e12, 1e12, 1e12, 1e12), [40, 24], 3, 50, 16, repeats=1)
+    after = answers()
+    assert all(torch.equal(before[k], after[k]) for k in before)
