@@ -141,9 +141,11 @@ def roofline(model: wl.Model, hw: wl.Hardware, tokens: float, pairs: float, keys
 
 
 def nominal(model: wl.Model, hw: wl.Hardware, prompts, batch: int, context: int):
-    """(prefill, decode) seconds of a layer at the record's rates: a pass over `prompts`, a step of `batch` tokens at `context`."""
-    n, s = len(prompts), max(1, round(sum(prompts) / len(prompts)))      # prompts of their mean length
-    return (roofline(model, hw, n * s, n * s * s, n * s), roofline(model, hw, batch, batch * context, batch * context))
+    """(prefill, decode) seconds, at the record's rates, of what the passes do: a pass over prompts of these lengths, whose queries see
+    themselves and the keys before them (the sweep's model counts every pair of a prompt), and a step of `batch` tokens at
+    `context`."""
+    tokens, pairs = sum(prompts), sum(n * (n + 1) / 2 for n in prompts)
+    return roofline(model, hw, tokens, pairs, tokens), roofline(model, hw, batch, batch * context, batch * context)
 
 
 def efficiency_samples(ctx: guide.Context, model: wl.Model, hw: wl.Hardware, prompts, batch: int, context: int, kv_block: int = 32,

@@ -19,3 +19,14 @@ def test_roofline_is_the_models(ora, model, batch, s_in):
         prefill = measure.roofline(model, hw, batch * s_in, batch * s_in ** 2, batch * s_in) + head(batch)
         decode = measure.roofline(model, hw, batch, batch * (s_in + 1), batch * (s_in + 1)) + head(batch)
         np.testing.assert_allclose([prefill, decode], [want["t_prefill"][0], want["t_decode"][0]], rtol=1e-12)
+
+
+def test_prompts_count_at_their_own_lengths():
+    """Where operations are all that costs, a pass over prompts costs the products' and the visible pairs'."""
+    m, hw = wl.DENSE_70B, wl.Hardware(1e15, 1e30, 1e12, 1e12)
+    d_h = m.d // m.n_h
+    product = 2 * (m.d * (m.n_h + 2 * m.n_kv) * d_h + m.n_h * d_h * m.d + 3 * m.d * m.d_ff)
+    for prompts in ([1], [100, 8000], [700, 300, 1048], [5] * 40):
+        visible = sum(i + 1 for n in prompts for i in range(n))
+        want = (sum(prompts) * product + visible * 4 * m.n_h * d_h) / hw.peak_flops
+        np.testing.assert_allclose(measure.nominal(m, hw, prompts, 1, 1)[0], want, rtol=1e-12)
