@@ -3,8 +3,9 @@
 The performance model prices a layer's tasks at a card's peak and bandwidth, which a sweep multiplies by efficiency samples
 (e_c, e_b).  This module runs those tasks -- norms, products with 4-bit weights, prompt attention, a paged 4-bit KV cache and
 the attention of single tokens over it -- at a shape of the user's, and compares the time of a prefill pass and of a decode
-pass with the performance model's price of the same layer: e_c is the ratio for the prefill pass (compute bound), e_b for the
-decode pass (bandwidth bound).  The pairs go into Context.eval_grid(e_c=..., e_b=...).
+pass with what the model's tasks would take at the record's rates for the work that these passes do (their own prompts, weights
+and cache in 4 bits): e_c is the ratio for the prefill pass (compute bound), e_b for the decode pass (bandwidth bound).  The
+pairs go into Context.eval_grid(e_c=..., e_b=...), whose configurations have the model's own widths.
 
     python -m paper_2412_04788_amd.measure --model dense-7b --prompts 700,300,1048 --batch 16 --context 4096
 """
@@ -18,6 +19,7 @@ import torch
 from . import guide, workloads as wl
 
 EPS = 1e-5
+HELD = 17 / 32           # bytes of a value in 4-bit codes with a scale per 32
 
 
 def _codes(rows: int, cols: int, bits: int):
@@ -127,7 +129,8 @@ def _seconds(run, repeats: int):
 
 def roofline(model: wl.Model, hw: wl.Hardware, tokens: float, pairs: float, keys: float, weight_bytes: float = 0.5, kv_bytes: float = 2.0):
     """Seconds of one dense layer's tasks on one GPU at the record's rates, as guide.h's performance model has them (roofline): a pass
-    over `tokens` tokens with `pairs` query-key pairs that reads `keys` cached tokens."""
+    over `tokens` tokens with `pairs` query-key pairs that reads `keys` cached tokens.  The widths, in bytes of a weight and of a
+    cached element, are the model's at wbits = 4 unless others are given; activations are two bytes."""
     d, d_h, t = model.d, model.d // model.n_h, tokens
     dq, dkv, ff = model.n_h * d_h, model.n_kv * d_h, model.d_ff
     w = lambda n: weight_bytes * n  # noqa: E731
@@ -143,9 +146,9 @@ def roofline(model: wl.Model, hw: wl.Hardware, tokens: float, pairs: float, keys
 def nominal(model: wl.Model, hw: wl.Hardware, prompts, batch: int, context: int):
     """(prefill, decode) seconds, at the record's rates, of what the passes do: a pass over prompts of these lengths, whose queries see
     themselves and the keys before them (the sweep's model counts every pair of a prompt), and a step of `batch` tokens at
-    `context`."""
+    `context` that reads its cache in 4 bits (the sweep's model: two bytes an element)."""
     tokens, pairs = sum(prompts), sum(n * (n + 1) / 2 for n in prompts)
-    return roofline(model, hw, tokens, pairs, tokens), roofline(model, hw, batch, batch * context, batch * context)
+    return (roofline(model, hw, tokens, pairs, tokens, HELD), roofline(model, hw, batch, batch * context, batch * context, HELD, HELD))
 
 
 def efficiency_samples(ctx: guide.Context, model: wl.Model, hw: wl.Hardware, prompts, batch: int, context: int, kv_block: int = 32,

@@ -30,3 +30,17 @@ def test_prompts_count_at_their_own_lengths():
         visible = sum(i + 1 for n in prompts for i in range(n))
         want = (sum(prompts) * product + visible * 4 * m.n_h * d_h) / hw.peak_flops
         np.testing.assert_allclose(measure.nominal(m, hw, prompts, 1, 1)[0], want, rtol=1e-12)
+
+
+def test_a_decode_step_is_priced_at_the_bytes_that_it_moves():
+    """Where bytes are all that costs: weights and cached tokens at 17 / 32 of a byte a value, as their buffers are large."""
+    from paper_2412_04788_amd import guide
+    m, hw, batch, context, block = wl.DENSE_7B, wl.Hardware(1e30, 5e12, 1e12, 1e12), 16, 4096, 32
+    table, pages = measure.page_tables([context] * batch, block)
+    d_h, t = m.d // m.n_h, batch
+    cache = pages * m.n_kv * 2 * block * (d_h // 2 + d_h // 32)
+    weights = sum(n * (k // 2 + k // guide.MX_GROUP) for n, k in (((m.n_h + 2 * m.n_kv) * d_h, m.d), (m.d, m.n_h * d_h), (2 * m.d_ff, m.d), (m.d, m.d_ff)))
+    # activations of two bytes: into and out of every product, q and o of the attention, four passes over the norms
+    acts = 2 * t * ((m.d + (m.n_h + 2 * m.n_kv) * d_h) + 2 * m.n_h * d_h + (m.n_h * d_h + m.d) + (m.d + 2 * m.d_ff) + (m.d_ff + m.d) + 4 * m.d)
+    want = (cache + weights + acts) / hw.hbm_bw
+    np.testing.assert_allclose(measure.nominal(m, hw, [1], batch, context)[1], want, rtol=1e-12)
