@@ -1,6 +1,7 @@
 """How the layer operators are called: tensors of one row or token as torch leaves them, streams, captured calls."""
 import math
 
+import numpy as np
 import pytest
 
 from tests import layer_ref as ref
@@ -91,3 +92,22 @@ def test_measuring_leaves_the_context_alone(ctx):
     measure.efficiency_samples(ctx, small, wl.Hardware(1e12, 1e12, 1e12, 1e12), [40, 24], 3, 50, 16, repeats=1)
     after = answers()
     assert all(torch.equal(before[k], after[k]) for k in before)
+
+
+def test_measured_times_are_the_cards(ctx):
+    """What the host does between the calls of a pass is not in its times; a pass of more work takes longer."""
+    import time
+    import torch
+    from paper_2412_04788_amd import measure
+    x = torch.randn(4096, 4096, device="cuda").bfloat16()
+    codes, scales = _buffers(torch, 4096, 4096, 4)
+
+    def run(times):
+        def call():
+            for _ in range(times):
+                time.sleep(0.02)
+                ctx.quantise(x, codes, scales, bits=4)
+        return call
+    one, many = measure._seconds(run(1), 5), measure._seconds(run(10), 5)
+    assert one.shape == many.shape == (5,)
+    assert (one > 0).all() and np.median(many) < 0.02 and np.median(many) > 3 * np.median(one)
