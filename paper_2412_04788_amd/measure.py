@@ -19,6 +19,7 @@ import torch
 from . import guide, workloads as wl
 
 EPS = 1e-5
+CARD = wl.Hardware(2.5e15, 8.0e12, 288 * wl.GIB, 1.53e11)     # MI355X: dense 16-bit matrix rate, HBM3E, one xGMI link
 HELD = 17 / 32           # bytes of a value in 4-bit codes with a scale per 32
 
 
@@ -198,7 +199,8 @@ def efficiency_samples(ctx: guide.Context, model: wl.Model, hw: wl.Hardware, pro
                 e_b=m_decode / t_decode)
 
 
-def main():
+def arguments(argv=None):
+    """(options, hardware record) of the command line."""
     ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     ap.add_argument("--model", default=wl.DENSE_7B.name, choices=[m.name for m in wl.MODELS_FULL if m.E == 1])
     ap.add_argument("--prompts", default="700,300,1048", help="prompt lengths of the prefill pass")
@@ -206,9 +208,18 @@ def main():
     ap.add_argument("--context", type=int, default=4096, help="cached tokens of a sequence in the decode pass, the new one among them")
     ap.add_argument("--kv-block", type=int, default=32)
     ap.add_argument("--repeats", type=int, default=16)
-    a = ap.parse_args()
+    ap.add_argument("--peak", type=float, default=CARD.peak_flops, help="FLOP/s of the record that the samples are relative to (the sweep's)")
+    ap.add_argument("--bandwidth", type=float, default=CARD.hbm_bw, help="its bytes/s")
+    a = ap.parse_args(argv)
+    if not a.peak > 0 or not a.bandwidth > 0:
+        ap.error("--peak and --bandwidth are above zero")
+    return a, wl.Hardware(a.peak, a.bandwidth, CARD.cap_bytes, CARD.link_bw)
+
+
+def main():
+    a, hw = arguments()
     model, = [m for m in wl.MODELS_FULL if m.name == a.model]
-    ctx, hw = guide.Context(0), wl.HW_TINY
+    ctx = guide.Context(0)
     got = efficiency_samples(ctx, model, hw, [int(n) for n in a.prompts.split(",")], a.batch, a.context, a.kv_block, a.repeats)
     for name in ("prefill", "decode"):
         print(f"{name}: median {np.median(got['t_' + name]) * 1e6:.1f} us a layer, {got['m_' + name] * 1e6:.1f} us at the record's nominal rates")

@@ -44,3 +44,12 @@ def test_a_decode_step_is_priced_at_the_bytes_that_it_moves():
     acts = 2 * t * ((m.d + (m.n_h + 2 * m.n_kv) * d_h) + 2 * m.n_h * d_h + (m.n_h * d_h + m.d) + (m.d + 2 * m.d_ff) + (m.d_ff + m.d) + 4 * m.d)
     want = (cache + weights + acts) / hw.hbm_bw
     np.testing.assert_allclose(measure.nominal(m, hw, [1], batch, context)[1], want, rtol=1e-12)
+
+
+def test_the_command_measures_against_a_record_of_the_users():
+    assert measure.arguments([])[1] == measure.CARD
+    a, hw = measure.arguments(["--peak", "1e15", "--bandwidth", "5e12", "--batch", "3"])
+    assert (hw.peak_flops, hw.hbm_bw, a.batch) == (1e15, 5e12, 3)
+    for bad in (["--peak", "0"], ["--bandwidth", "-1"], ["--bandwidth", "nan"]):
+        with pytest.raises(SystemExit):
+            measure.arguments(bad)
