@@ -207,12 +207,14 @@ def arguments(argv=None):
     ap.add_argument("--batch", type=int, default=16)
     ap.add_argument("--context", type=int, default=4096, help="cached tokens of a sequence in the decode pass, the new one among them")
     ap.add_argument("--kv-block", type=int, default=32)
-    ap.add_argument("--repeats", type=int, default=16)
+    ap.add_argument("--repeats", type=int, default=16, help="samples, 2 to 64 (what a sweep takes)")
     ap.add_argument("--peak", type=float, default=CARD.peak_flops, help="FLOP/s of the record that the samples are relative to (the sweep's)")
     ap.add_argument("--bandwidth", type=float, default=CARD.hbm_bw, help="its bytes/s")
     a = ap.parse_args(argv)
     if not a.peak > 0 or not a.bandwidth > 0:
         ap.error("--peak and --bandwidth are above zero")
+    if not 2 <= a.repeats <= 64:
+        ap.error("--repeats: 2 to 64")
     return a, wl.Hardware(a.peak, a.bandwidth, CARD.cap_bytes, CARD.link_bw)
 
 

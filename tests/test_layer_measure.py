@@ -53,3 +53,10 @@ def test_the_command_measures_against_a_record_of_the_users():
     for bad in (["--peak", "0"], ["--bandwidth", "-1"], ["--bandwidth", "nan"]):
         with pytest.raises(SystemExit):
             measure.arguments(bad)
+
+
+def test_the_command_takes_as_many_samples_as_a_sweep():
+    assert measure.arguments(["--repeats", "64"])[0].repeats == 64
+    for bad in ("1", "65"):
+        with pytest.raises(SystemExit):
+            measure.arguments(["--repeats", bad])
