@@ -160,8 +160,8 @@ struct Rows {
         for (int j = 0; j < 32; j += 2) {
             const float e0 = __builtin_amdgcn_exp2f(fmaf(sc[j / 16][j % 16], c, -base));          // 0 where masked
             const float e1 = __builtin_amdgcn_exp2f(fmaf(sc[j / 16][j % 16 + 1], c, -base));
-            part_sum[j / 8] += e0 + e1;
             pp[j / 2] = __builtin_convertvector(f32x2{e0, e1}, typename Mat<T>::v2);
+            part_sum[j / 8] = Mat<T>::sum2(pp[j / 2], part_sum[j / 8]);
         }
         sum += (part_sum[0] + part_sum[1]) + (part_sum[2] + part_sum[3]);
         __builtin_memcpy(p, pp, sizeof p);
