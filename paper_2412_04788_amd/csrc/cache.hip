@@ -230,10 +230,10 @@ __global__ __launch_bounds__(kBlock, 3) void cache_attention_kernel(CacheView c,
         float e[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) e[j] = __builtin_amdgcn_exp2f(fmaf(sc[j / 4][j % 4], cs, -base));        // 0 where not seen
-        sum += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
         typename Mat<T>::v2 pp[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) pp[j] = __builtin_convertvector(f32x2{e[2 * j], e[2 * j + 1]}, typename Mat<T>::v2);
+        sum += Mat<T>::sum2(pp[0], Mat<T>::sum2(pp[1], 0.0f)) + Mat<T>::sum2(pp[2], Mat<T>::sum2(pp[3], 0.0f));
         V8 pf;
         __builtin_memcpy(&pf, pp, 16);
         float f[8];

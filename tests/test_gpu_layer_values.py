@@ -31,3 +31,28 @@ def test_prompt_greatest_values(ctx, heads, kv, d, nq, nk):
     out = torch.zeros_like(q)
     ctx.prompt_attention(q, k, v, _starts(torch, [nq]), _starts(torch, [nk]), out, scale=1.0)
     assert (out[..., ::2] == 65504).all() and (out[..., 1::2] == -65504).all()
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("heads,kv,d,n", [(4, 2, 64, 300), (17, 1, 128, 300), (4, 1, 128, 9000)])
+def test_cache_mean_of_equal_values(ctx, dtype, heads, kv, d, n):
+    """A mean of equal values is that value, by one block and by many, with probabilities that are rounded up."""
+    import torch
+    dt, block = getattr(torch, dtype), 32
+    # keys of 0 and of -1, a query of 1: the scale is the score against the latter, its exponential just past a tie above 1/2
+    scale = -math.log(0.5 + 1.02 * 2.0 ** (-9 if dt == torch.bfloat16 else -12))
+    q = torch.zeros(1, heads, d, dtype=dt, device="cuda")
+    q[..., 0] = 1
+    k, v = torch.zeros(n, kv, d, dtype=dt, device="cuda"), torch.full((n, kv, d), 1.5, dtype=dt, device="cuda")
+    k[..., 0] = -1
+    k[::32, :, 0] = 0                                        # (one in every tile)
+    pages = -(-n // block)
+    codes = torch.zeros(pages, kv, 2, block, d // 2, dtype=torch.uint8, device="cuda")
+    scales = torch.zeros(pages, kv, 2, d // 32, block, dtype=torch.uint8, device="cuda")
+    ctx.cache_append(k, v, torch.arange(n, device="cuda"), codes, scales)
+    table = torch.arange(pages, dtype=torch.int32, device="cuda").view(1, pages)
+    out = torch.zeros_like(q)
+    need = ctx.cache_attention_workspace_bytes(1, heads, kv, d, pages * block)
+    ctx.cache_attention(q, codes, scales, table, torch.tensor([n], dtype=torch.int32, device="cuda"), out,
+                        torch.empty(need, dtype=torch.uint8, device="cuda") if need else None, scale=scale)
+    assert (out == 1.5).all()
