@@ -167,10 +167,18 @@ struct Rows {
         __builtin_memcpy(p, pp, sizeof p);
     }
 
-    // A value that is no finite number reaches the rows that see its key and no others: 0 times it would be a NaN.  Adds those
-    // of keys k0 .. that the row sees; values<true> leaves them out.
+    // A value that is no finite number reaches the rows that see its key and no others: 0 times it would be a NaN.  Adds the products
+    // with those of keys k0 .. that the row sees; values<true> leaves them out.
     __device__ __forceinline__ void add_odd(int k0, const uint8_t *lds_v) {
-        for (int r = 0; r < kTileK; ++r)
+        uint32_t pairs[16];
+        __builtin_memcpy(pairs, p, sizeof pairs);
+        for (int r = 0; r < kTileK; ++r) {
+            const int j = r / 8 * 4 + r % 4;                         // the key's probability is number j of half r / 4 % 2
+            uint32_t pair = pairs[0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) pair = j / 2 == i ? pairs[i] : pair;
+            const auto two = __builtin_bit_cast(typename Mat<T>::v2, pair);
+            const float weight = __shfl((float)(j % 2 ? two[1] : two[0]), lane % 32 + r / 4 % 2 * 32);
 #pragma unroll
             for (int i = 0; i < D / 32; ++i)
 #pragma unroll
@@ -179,8 +187,9 @@ struct Rows {
                     __builtin_memcpy(x, lds_v + r * kRow + piece_of<D, false>(r, i * 4 + a) * 16 + half * 8, 8);
 #pragma unroll
                     for (int b = 0; b < 4; ++b)
-                        if (k0 + r < sees && !__builtin_isfinite((float)x[b])) o[i][a * 4 + b] += (float)x[b];
+                        if (k0 + r < sees && !__builtin_isfinite((float)x[b])) o[i][a * 4 + b] += weight * (float)x[b];
                 }
+        }
     }
 
     // O' += V' P'.  V' of channels 32 i .. comes by transposing reads: a group of 16 lanes reads four keys' 16 channels and gets,

@@ -56,3 +56,26 @@ def test_cache_mean_of_equal_values(ctx, dtype, heads, kv, d, n):
     ctx.cache_attention(q, codes, scales, table, torch.tensor([n], dtype=torch.int32, device="cuda"), out,
                         torch.empty(need, dtype=torch.uint8, device="cuda") if need else None, scale=scale)
     assert (out == 1.5).all()
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("heads,kv,d,nq,nk,at", [(4, 2, 64, 700, 700, 5), (4, 2, 128, 700, 700, 300), (2, 1, 128, 3, 5000, 100), (2, 1, 64, 3, 5000, 4999),
+                                                 (128, 8, 128, 512, 5000, 5), (128, 8, 128, 512, 5000, 4900)])
+@pytest.mark.parametrize("score", [0.0, -200.0])
+def test_prompt_infinite_value(ctx, dtype, heads, kv, d, nq, nk, at, score):
+    """An infinity gives every row that sees it the same, whether the row sees all of the key's tile or not: an infinity, or a NaN
+    where its probability is zero."""
+    import torch
+    dt = getattr(torch, dtype)
+    q, k, v = (torch.zeros(n, h, d, dtype=dt, device="cuda") for n, h in ((nq, heads), (nk, kv), (nk, kv)))
+    q[..., 0], k[at, :, 0] = 1, score
+    k[at, 0, 0] = 0                                                # (not for the heads of the first KV head)
+    v[at, :, 3], v[at, :, d - 1] = math.inf, -math.inf
+    out = torch.zeros_like(q)
+    ctx.prompt_attention(q, k, v, _starts(torch, [nq]), _starts(torch, [nk]), out, scale=1.0)
+    sees = torch.arange(nq, device="cuda") + nk - nq >= at
+    want = torch.zeros_like(out)
+    want[sees, :, 3], want[sees, :, d - 1] = math.inf, -math.inf
+    if score < 0:
+        want[sees, heads // kv:, 3], want[sees, heads // kv:, d - 1] = math.nan, math.nan
+    assert torch.equal(out.isnan(), want.isnan()) and torch.equal(out.nan_to_num(1), want.nan_to_num(1))
