@@ -76,21 +76,34 @@ __global__ __launch_bounds__(kBlock) void cache_tokens_kernel(CacheView c, guide
     }
 }
 
-constexpr uint32_t kBlocksWanted = 4096, kLeastChunk = 512;
+constexpr uint32_t kBlocksWanted = 4096, kBlocksAtOnce = 1024, kLeastChunk = 512;
 
 // How the keys of a sequence are split: up to `chunk` keys to a block.  A block's four waves take 32 keys at a time; the chip runs
 // 1024 blocks at once, and four times as many even out sequences of different lengths; a block of fewer than 512 keys is mostly
-// start and end.
-struct Split { uint32_t chunk, splits; };
+// start and end.  A chunk follows from the table's width, which may be far more than any sequence has: so a sequence uses at least
+// as many blocks as would fill the chip if all were like it (`fill`), of 512 keys or more.  16 sequences of 4000 tokens, 32 heads on
+// 8: 20 us with a table for 4000 tokens, 21 with one for 131 072 (35 in chunks of its width).
+struct Split {
+    uint32_t chunk, fill, splits;                                    // splits: the most that a sequence can use
+
+    __host__ __device__ uint32_t used(uint32_t length) const {       // (one where there is nothing: it writes what an empty sequence gives)
+        const uint32_t even = (length + chunk - 1) / chunk, least = (length + kLeastChunk - 1) / kLeastChunk;
+        const uint32_t filling = least < fill ? least : fill, n = even > filling ? even : filling;
+        return n ? n : 1;
+    }
+};
 
 Split split_of(uint32_t n_seq, uint32_t n_h, uint32_t n_kv, uint64_t max_len) {
-    const uint64_t rows = (uint64_t)n_seq * n_kv * ((n_h / n_kv + 15) / 16);
-    uint64_t want = kBlocksWanted / (rows ? rows : 1);
+    const uint64_t all = (uint64_t)n_seq * n_kv * ((n_h / n_kv + 15) / 16), rows = all ? all : 1;
+    if (max_len > (1u << 30)) max_len = 1u << 30;                    // (a call takes no more)
+    uint64_t want = kBlocksWanted / rows;
     if (want < 1) want = 1;
     uint64_t chunk = (max_len + want - 1) / want;
     if (chunk < kLeastChunk) chunk = kLeastChunk;
     chunk = (chunk + 127) / 128 * 128;
-    return {(uint32_t)chunk, (uint32_t)((max_len + chunk - 1) / chunk)};
+    Split sp = {(uint32_t)chunk, (uint32_t)(kBlocksAtOnce / rows), 1};
+    sp.splits = sp.used((uint32_t)max_len);
+    return sp;
 }
 
 // Partial results of (sequence, head, split): the maximum and the sum of its softmax, then the weighted values.
@@ -107,9 +120,6 @@ __device__ inline uint32_t length_of(const guide_cache_queries &s, uint32_t bloc
     const int32_t asked = s.lengths[seq];
     return asked < 0 ? 0u : min((uint32_t)asked, s.max_pages * block);
 }
-
-// Splits of a sequence (one where there is nothing: it writes what an empty sequence gives).
-__device__ inline uint32_t splits_used(uint32_t length, uint32_t chunk) { return max(1u, (length + chunk - 1) / chunk); }
 
 // Two neighbouring values of the codes in byte B of w, times the scale whose exponent field is that of f (0 = 2^-127, 255 = NaN).
 template <int T, int B>
@@ -135,8 +145,7 @@ struct Piece {
 // Bound by memory: 64 sequences of 1000 to 16 000 tokens, 64 heads on 8 of 128, 87 us (381 MB, 4.4 TB/s) and 5.5 for the join; of
 // one sequence of 40 001 tokens (43.5 MB) 13 us, 4 of them until the first keys arrive.
 template <int T, int D>
-__global__ __launch_bounds__(kBlock, 3) void cache_attention_kernel(CacheView c, guide_cache_queries s, Div32 by_block, uint32_t chunk,
-                                                                    uint32_t splits, void *ws) {
+__global__ __launch_bounds__(kBlock, 3) void cache_attention_kernel(CacheView c, guide_cache_queries s, Div32 by_block, Split sp, void *ws) {
     using E = typename Elem<T>::type;
     using V8 = typename Mat<T>::v8;
     constexpr int kGroups = D / 32;                                  // scale groups of a token
@@ -147,7 +156,7 @@ __global__ __launch_bounds__(kBlock, 3) void cache_attention_kernel(CacheView c,
     // (heads first, splits last: blocks go round the eight XCDs in turn, and late splits are those of long sequences only)
     const uint32_t split = blockIdx.z, seq = blockIdx.y, kv = blockIdx.x / tiles, tile = blockIdx.x % tiles;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, quarter = lane / 16;
-    const uint32_t length = length_of(s, c.block, seq), used = splits_used(length, chunk);
+    const uint32_t length = length_of(s, c.block, seq), used = sp.used(length), splits = sp.splits;
     if (split >= used) return;
     const uint32_t share = ((length + used - 1) / used + 31) / 32 * 32;      // the sequence's splits are even ones, of whole tiles
     const uint32_t begin = min(split * share, length), end = min(begin + share, length);
@@ -322,14 +331,14 @@ __global__ __launch_bounds__(kBlock, 3) void cache_attention_kernel(CacheView c,
 // split i goes to strand i modulo their number, and the strands are joined in a fixed order.  Bound by latency: a strand's first
 // four splits are loaded before anything is known about them (in bounds, and left out of the sums if they were not written).
 template <int T, int D, int WAVES>
-__global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : kBlock) void cache_join_kernel(guide_cache_queries s, uint32_t block, uint32_t chunk, uint32_t splits,
+__global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : kBlock) void cache_join_kernel(guide_cache_queries s, uint32_t block, Split sp,
                                                                                       uint32_t rows, const void *ws) {
     using E = typename Elem<T>::type;
     constexpr int kStrands = WAVES * 256 / D;                        // of a row
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, ch = lane % (D / 4) * 4;
     const uint32_t row = WAVES == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
     if (WAVES == 1 && row >= rows) return;
-    const uint32_t seq = row / s.n_h, head = row - seq * s.n_h;
+    const uint32_t seq = row / s.n_h, head = row - seq * s.n_h, splits = sp.splits;
     const Partials part((void *)ws, (size_t)rows * splits);
     const size_t at = (size_t)row * splits;
     const uint32_t strand = (WAVES == 1 ? 0 : wave * (256 / D)) + lane / (D / 4);
@@ -345,7 +354,7 @@ __global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : kBlock) void cache_join_ke
     };
     load(strand);
     float best = -INFINITY;
-    const uint32_t used = splits_used(length_of(s, block, seq), chunk);
+    const uint32_t used = sp.used(length_of(s, block, seq));
     for (uint32_t i = lane; i < used; i += 64) best = fmaxf(best, part.top[at + i]);
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) best = fmaxf(best, __shfl_xor(best, m));
@@ -414,13 +423,13 @@ hipError_t tokens_any(const guide_cache &c, const guide_cache_tokens &t, hipStre
 template <int T, int D>
 hipError_t attention_as(const guide_cache &c, const guide_cache_queries &q, void *ws, hipStream_t stream) {
     const Split sp = split_of(q.n_seq, q.n_h, c.n_kv, (uint64_t)q.max_pages * c.kv_block);
-    const uint32_t splits = sp.splits ? sp.splits : 1, tiles = (q.n_h / c.n_kv + 15) / 16;
-    cache_attention_kernel<T, D><<<dim3(c.n_kv * tiles, q.n_seq, splits), kBlock, 0, stream>>>(view_of(c), q, make_div32(c.kv_block), sp.chunk, splits, ws);
+    const uint32_t splits = sp.splits, tiles = (q.n_h / c.n_kv + 15) / 16;
+    cache_attention_kernel<T, D><<<dim3(c.n_kv * tiles, q.n_seq, splits), kBlock, 0, stream>>>(view_of(c), q, make_div32(c.kv_block), sp, ws);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || splits == 1) return e;
     const uint32_t rows = q.n_seq * q.n_h;                           // (a wave to a row where a strand has a few splits at most)
-    if (splits <= 16) cache_join_kernel<T, D, 1><<<(rows + 3) / 4, kBlock, 0, stream>>>(q, c.kv_block, sp.chunk, splits, rows, ws);
-    else cache_join_kernel<T, D, 16><<<rows, 1024, 0, stream>>>(q, c.kv_block, sp.chunk, splits, rows, ws);
+    if (splits <= 16) cache_join_kernel<T, D, 1><<<(rows + 3) / 4, kBlock, 0, stream>>>(q, c.kv_block, sp, rows, ws);
+    else cache_join_kernel<T, D, 16><<<rows, 1024, 0, stream>>>(q, c.kv_block, sp, rows, ws);
     return hipGetLastError();
 }
 

@@ -111,3 +111,24 @@ def test_measured_times_are_the_cards(ctx):
     one, many = measure._seconds(run(1), 5), measure._seconds(run(10), 5)
     assert one.shape == many.shape == (5,)
     assert (one > 0).all() and np.median(many) < 0.02 and np.median(many) > 3 * np.median(one)
+
+
+@pytest.mark.parametrize("seqs,length", [(16, 4000), (1, 700), (3, 513), (2, 0)])
+def test_cache_attention_is_split_by_lengths_not_by_tables(ctx, seqs, length):
+    """With a table of 131 072 tokens a sequence's keys go to as many blocks as with one that it fills: so many parts of every row are
+    written to the workspace, which starts with the parts' maxima."""
+    import torch
+    kv, heads, d, block = 8, 32, 128, 32
+    pages = -(-max(length, 1) // block)
+    codes = torch.full((pages, kv, 2, block, d // 2), 0x22, dtype=torch.uint8, device="cuda")
+    scales = torch.full((pages, kv, 2, d // 32, block), 127, dtype=torch.uint8, device="cuda")
+    q, lengths = torch.ones(seqs, heads, d, device="cuda").bfloat16(), torch.full((seqs,), length, dtype=torch.int32, device="cuda")
+    for width in (pages, 4096):
+        table = torch.arange(pages, dtype=torch.int32, device="cuda").repeat(seqs, -(-width // pages))[:, :width].contiguous()
+        need, out = ctx.cache_attention_workspace_bytes(seqs, heads, kv, d, width * block), torch.zeros_like(q)
+        room = torch.full((max(need // 4, 1),), math.nan, device="cuda")
+        ctx.cache_attention(q, codes, scales, table, lengths, out, room)
+        assert (out == (1 if length else 0)).all()
+        parts = (~room[:need // (4 * (d + 2))].view(seqs * heads, -1).isnan()).sum(1)
+        if need:
+            assert (parts == max(1, -(-length // 512))).all(), (width, parts)
