@@ -10,14 +10,26 @@ namespace {
 
 constexpr int kRowsPerWave = 32;
 
-// The sequence and the tile in it that tile number `tile` of the packed queries is (sequences have ceil(n_q / ROWS)
-// tiles each); false when there are fewer tiles.  Every lane of a wave looks at one sequence at a time.
-struct Place { uint32_t q0, nq, k0, nk, tile; };
+// How the keys of a sequence are split over blocks: into as many parts as `size` goes into the number of keys that its queries see on
+// average, at most `most` of them, or `many` where it has several tiles of queries.
+struct Cut {
+    Div32 size;
+    uint32_t most, many;
+    __device__ uint32_t parts(uint32_t nq, uint32_t nk) const {
+        const uint32_t seen = nk > nq / 2 ? nk - nq / 2 : 0;
+        return max(1u, min(div32(seen, size), nq > 4 * kRowsPerWave ? many : most));
+    }
+};
+
+// The sequence, the tile in it and the part of its keys that unit number `unit` of the packed queries is (sequences have
+// ceil(n_q / ROWS) tiles each, and without a cut a tile is a unit); false when there are fewer units.  Every lane of a wave looks
+// at one sequence at a time.
+struct Place { uint32_t q0, nq, k0, nk, tile, part, parts; };
 
 __device__ inline uint32_t clamped(int32_t v, uint32_t total) { return v < 0 ? 0u : (uint32_t)v > total ? total : (uint32_t)v; }
 
-template <int ROWS>
-__device__ inline bool find_tile(const guide_prompt_spec &s, uint32_t tile, Place &p) {
+template <int ROWS, bool SPLIT>
+__device__ inline bool find_unit(const guide_prompt_spec &s, const Cut &cut, uint32_t unit, Place &p) {
     const uint32_t lane = threadIdx.x % 64;
     uint32_t before = 0;
     for (uint32_t s0 = 0; s0 < s.n_seq; s0 += 64) {
@@ -29,21 +41,24 @@ __device__ inline bool find_tile(const guide_prompt_spec &s, uint32_t tile, Plac
             k0 = clamped(s.k_starts[q], s.total_k);
             k1 = clamped(s.k_starts[q + 1], s.total_k);
         }
-        const uint32_t tiles = b > a ? (b - a + ROWS - 1) / ROWS : 0;
-        uint32_t sum = tiles;                                        // running sum over the lanes
+        const uint32_t nk = k1 > k0 ? k1 - k0 : 0, parts = SPLIT && b > a ? cut.parts(b - a, nk) : 1;
+        const uint32_t units = b > a ? (b - a + ROWS - 1) / ROWS * parts : 0;
+        uint32_t sum = units;                                        // running sum over the lanes
 #pragma unroll
         for (int m = 1; m < 64; m <<= 1) {
             const uint32_t o = __shfl_up(sum, m);
             if ((int)lane >= m) sum += o;
         }
-        const uint64_t past = __ballot(before + sum > tile);
+        const uint64_t past = __ballot(before + sum > unit);
         if (past) {
             const int w = __builtin_ctzll(past);
-            p.q0 = (uint32_t)__builtin_amdgcn_readlane((int)a, w);
-            p.nq = (uint32_t)__builtin_amdgcn_readlane((int)b, w) - p.q0;
-            p.tile = tile - (before + (uint32_t)__builtin_amdgcn_readlane((int)(sum - tiles), w));
-            p.k0 = (uint32_t)__builtin_amdgcn_readlane((int)k0, w);
-            p.nk = (uint32_t)__builtin_amdgcn_readlane((int)(k1 > k0 ? k1 - k0 : 0), w);
+            auto of = [&](uint32_t x) __attribute__((always_inline)) { return (uint32_t)__builtin_amdgcn_readlane((int)x, w); };
+            p.q0 = of(a), p.nq = of(b) - p.q0, p.k0 = of(k0), p.nk = of(nk);
+            p.tile = unit - (before + of(sum - units)), p.part = 0, p.parts = 1;
+            if constexpr (SPLIT) {
+                p.parts = of(parts);
+                p.part = p.tile % p.parts, p.tile /= p.parts;
+            }
             return true;
         }
         before += (uint32_t)__builtin_amdgcn_readlane((int)sum, 63);
@@ -258,23 +273,23 @@ struct Rows {
     }
 };
 
-// What a block works on: one head's queries of one tile.  Late tiles, which see the most keys, come first.  Blocks go round
-// the eight XCDs in turn: with a multiple of eight KV heads, the query heads of one KV head stay on one XCD, whose L2 then
-// holds its keys once.
-template <int ROWS>
-__device__ __forceinline__ bool find_work(const guide_prompt_spec &s, uint32_t tiles, Place &p, uint32_t &head, uint32_t &kv) {
+// What a block works on: one head's queries of one tile, and a part of the keys.  Late tiles, which see the most keys, come first.
+// Blocks go round the eight XCDs in turn: with a multiple of eight KV heads, the query heads of one KV head stay on one XCD, whose L2
+// then holds its keys once.
+template <int ROWS, bool SPLIT>
+__device__ __forceinline__ bool find_work(const guide_prompt_spec &s, const Cut &cut, uint32_t units, Place &p, uint32_t &head, uint32_t &kv) {
     const uint32_t group = s.n_h / s.n_kv;
-    uint32_t tile;
+    uint32_t unit;
     if (s.n_kv % 8 == 0) {
         const uint32_t per = s.n_h / 8, x = blockIdx.x / 8, h = x % per;
         head = (blockIdx.x % 8 + 8 * (h / group)) * group + h % group;
-        tile = x / per;
+        unit = x / per;
     } else {
         head = blockIdx.x % s.n_h;
-        tile = blockIdx.x / s.n_h;
+        unit = blockIdx.x / s.n_h;
     }
     kv = head / group;
-    return find_tile<ROWS>(s, tiles - 1 - tile, p);
+    return find_unit<ROWS, SPLIT>(s, cut, units - 1 - unit, p);
 }
 
 // Whether the wave's part of a staged tile of values, which it sent for itself, holds an infinity or a NaN.
@@ -311,9 +326,10 @@ struct Parts {
 // way while one is worked on.  Two such blocks share a compute unit, so that one's exponentials run beside the other's products
 // (48 % of the matrix units' cycles in a pass of six prompts of 300 to 3900 tokens, 64 heads on 8 of 128: 440 us, 880 TFLOP/s of
 // visible pairs, and 3 % in vain in tiles that are partly masked; the waves of a block wait for its last one there).
-// SPLIT: block y of the grid's takes the y-th part of the keys that any of the queries sees, and prompt_join_kernel joins the parts.
+// SPLIT: a sequence of many keys gives every tile so many blocks, each of which takes its part of the keys that any of the queries sees,
+// and prompt_join_kernel joins the parts.
 template <int T, int D, bool SPLIT>
-__global__ __launch_bounds__(256, 2) void prompt_kernel(guide_prompt_spec s, uint32_t tiles, float *scratch) {
+__global__ __launch_bounds__(256, 2) void prompt_kernel(guide_prompt_spec s, uint32_t units, Cut cut, float *scratch) {
     using E = typename Elem<T>::type;
     constexpr int kRow = D * 2, kTileQ = 4 * kRowsPerWave;
     using SendK = Sender<D, true, 4>;
@@ -322,7 +338,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(guide_prompt_spec s, uin
     __shared__ uint32_t odd0[4], odd1[4];
     Place p;
     uint32_t head, kv;
-    if (!find_work<kTileQ>(s, tiles, p, head, kv)) return;
+    if (!find_work<kTileQ, SPLIT>(s, cut, units, p, head, kv)) return;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int first = (int)(p.tile * kTileQ) + wave * kRowsPerWave, row = first + lane % 32;      // queries of the sequence
     const int nq = (int)p.nq, nk = (int)p.nk, shift = nk - nq;
@@ -330,8 +346,8 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(guide_prompt_spec s, uin
     int last = min((int)p.tile * kTileQ + kTileQ, nq) + shift;                      // ... any row of the block
     int k0 = 0;
     if constexpr (SPLIT) {
-        const int part = (max(last, 0) / (int)gridDim.y + 2 * kTileK) / (2 * kTileK) * (2 * kTileK);      // whole pairs of tiles
-        k0 = min((int)blockIdx.y * part, (max(last, 0) + 2 * kTileK - 1) / (2 * kTileK) * (2 * kTileK));
+        const int part = (max(last, 0) / (int)p.parts + 2 * kTileK) / (2 * kTileK) * (2 * kTileK);      // whole pairs of tiles
+        k0 = min((int)p.part * part, (max(last, 0) + 2 * kTileK - 1) / (2 * kTileK) * (2 * kTileK));
         last = min(last, k0 + part);
     }
 
@@ -394,9 +410,9 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(guide_prompt_spec s, uin
         masked_step(k0 + kTileK, lds_k1, lds_v1, lds_k0, lds_v0, odd1);
     }
     arrived();                                                       // (no load may be on its way to the LDS of a block that has ended)
-    if constexpr (SPLIT) {
-        const Parts parts(scratch, (uint64_t)s.total_q * s.n_h, gridDim.y);
-        const uint64_t at = blockIdx.y * parts.rows + (uint64_t)(p.q0 + row) * s.n_h + head;
+    if (SPLIT && p.parts > 1) {
+        const Parts parts(scratch, (uint64_t)s.total_q * s.n_h, cut.most);
+        const uint64_t at = p.part * parts.rows + (uint64_t)(p.q0 + row) * s.n_h + head;
         const bool real = row < nq;
         rows.finish_part(real ? parts.top + at : nullptr, parts.sum + at, parts.value + at * D);
     } else {
@@ -420,7 +436,7 @@ __global__ __launch_bounds__(512, 2) void prompt_pair_kernel(guide_prompt_spec s
     __shared__ uint32_t odd0[8], odd1[8];
     Place p;
     uint32_t head, kv;
-    if (!find_work<kTileQ>(s, tiles, p, head, kv)) return;
+    if (!find_work<kTileQ, false>(s, Cut{}, tiles, p, head, kv)) return;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int first = (int)(p.tile * kTileQ) + wave * kRowsPerWave, row = first + lane % 32;
     const int nq = (int)p.nq, nk = (int)p.nk, shift = nk - nq;
@@ -523,20 +539,31 @@ __global__ __launch_bounds__(512, 2) void prompt_pair_kernel(guide_prompt_spec s
     rows.finish(row < nq ? (E *)s.out + (int64_t)(p.q0 + row) * s.out_stride + (int64_t)head * s.out_head_stride : nullptr);
 }
 
-// Joins the parts, in their order: D / 4 lanes to a row, four channels to a lane; blocks (x, y) take the rows of tile x in slices.
-// Bound by latency (4 to 5 us) until the parts are many megabytes.
-constexpr uint32_t kMostParts = 16;
+// Joins the parts of the rows that have several, in their order: a block takes some heads of one query, D / 4 lanes to a head, four
+// channels to a lane.  Bound by latency (4 to 5 us) until the parts are many megabytes.
+constexpr uint32_t kMostParts = 16, kWorth = 8192;
 template <int T, int D>
-__global__ __launch_bounds__(256) void prompt_join_kernel(guide_prompt_spec s, uint32_t tiles, const float *scratch, uint32_t count) {
+__global__ __launch_bounds__(256) void prompt_join_kernel(guide_prompt_spec s, Cut cut, const float *scratch) {
     using E = typename Elem<T>::type;
-    constexpr int kSlice = 256 / (D / 4);
-    Place p;
-    uint32_t head, kv;
-    if (!find_work<4 * kRowsPerWave>(s, tiles, p, head, kv)) return;
-    const uint32_t row = p.tile * 4 * kRowsPerWave + blockIdx.y * kSlice + threadIdx.x / (D / 4), ch = threadIdx.x % (D / 4) * 4;
-    if (row >= p.nq) return;
-    const Parts parts((float *)scratch, (uint64_t)s.total_q * s.n_h, count);
-    const uint64_t at = (uint64_t)(p.q0 + row) * s.n_h + head;
+    constexpr uint32_t kHeads = 256 / (D / 4);
+    const uint32_t groups = (s.n_h + kHeads - 1) / kHeads, query = blockIdx.x / groups;
+    const uint32_t head = blockIdx.x % groups * kHeads + threadIdx.x / (D / 4), ch = threadIdx.x % (D / 4) * 4;
+    uint32_t count = 0;
+    for (uint32_t s0 = 0; s0 < s.n_seq && count == 0; s0 += 64) {
+        const uint32_t q = s0 + threadIdx.x % 64;
+        uint32_t a = 0, b = 0, nk = 0;
+        if (q < s.n_seq) {
+            a = clamped(s.q_starts[q], s.total_q);
+            b = clamped(s.q_starts[q + 1], s.total_q);
+            const uint32_t k0 = clamped(s.k_starts[q], s.total_k), k1 = clamped(s.k_starts[q + 1], s.total_k);
+            nk = k1 > k0 ? k1 - k0 : 0;
+        }
+        const uint64_t here = __ballot(a <= query && query < b);
+        if (here) count = (uint32_t)__builtin_amdgcn_readlane((int)cut.parts(b - a, nk), __builtin_ctzll(here));
+    }
+    if (count < 2 || head >= s.n_h) return;
+    const Parts parts((float *)scratch, (uint64_t)s.total_q * s.n_h, cut.most);
+    const uint64_t at = (uint64_t)query * s.n_h + head;
     float top[kMostParts], sum[kMostParts];
     f32x4 v[kMostParts];
 #pragma unroll
@@ -561,7 +588,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(guide_prompt_spec s, u
     E e[4];
 #pragma unroll
     for (int b = 0; b < 4; ++b) e[b] = (E)(total != 0.0f ? x[b] / total : 0.0f);
-    __builtin_memcpy((E *)s.out + (int64_t)(p.q0 + row) * s.out_stride + (int64_t)head * s.out_head_stride + ch, e, 8);
+    __builtin_memcpy((E *)s.out + (int64_t)query * s.out_stride + (int64_t)head * s.out_head_stride + ch, e, 8);
 }
 
 // launch(tiles, blocks) for the blocks of all tiles times heads, the last tiles first, as many at a time as a launch holds:
@@ -594,25 +621,33 @@ hipError_t prompt_as(const guide_prompt_spec &s, float *scratch, hipStream_t str
         }
     }
     const uint32_t tiles = s.total_q / 128 + filled;                // at least as many as there are
-    // Too few tiles to give every compute unit two blocks: keys are split.  Whole / split, 32 heads on 8 of 128: 1 query over 8001 keys 135 /
-    // 26 us, 256 over 32 256 536 / 155, 512 over 8512 154 / 97.  Of the least number of keys to a part, 256 / 512: 1 over 1001 15.9 / 23.5,
-    // 64 over 1064 19.6 / 21.4; but with more rows to join, 128 over 2128 of 32 heads 29 / 26, 1500 over 1500 of 12 heads 37.7 / 32.2.
-    const uint64_t fewest = (uint64_t)((s.total_q + 127) / 128 > s.n_seq ? (s.total_q + 127) / 128 : s.n_seq) * s.n_h;
-    const uint64_t room = kScratch / ((uint64_t)s.total_q * s.n_h * (D + 2) * sizeof(float));
-    uint64_t parts = 2 * kNumCU / fewest;
-    for (const uint64_t most : {keys / ((uint64_t)s.total_q * s.n_h <= 2048 ? 256 : 512), room, (uint64_t)kMostParts}) parts = parts < most ? parts : most;
-    if (parts < 2) {
+    // Too little work to give every compute unit two blocks: keys are split, into parts of what two blocks to a unit would have of all of
+    // it.  Whole / split, 32 heads on 8 of 128: 1 query over 8001 keys 135 / 26 us, 256 over 32 256 536 / 155, 512 over 8512 154 / 90.
+    // Of the least number of keys to a part, 256 / 512: 1 over 1001 15.4 / 23.5, 64 over 1064 20.2 / 21.4; but with more rows to join,
+    // 128 over 2128 of 32 heads 29 / 24, 1500 over 1500 of 12 heads 37.7 / 32.2.
+    // Blocks enough, but for what is known here all keys may be one sequence's: sequences of one tile are split where their own keys ask
+    // for it.  One query each over 100 keys, 15 times, and 60 000: 990 / 122, with 64 heads 990 / 237; 16 over 100 to 8000 keys 155 /
+    // 100.  Where they are equal after all, that is for nothing (16 over 4000 each 125 / 133, 64 over 1000 of 64 heads 232 / 244), so it
+    // is done only where a sequence of all keys would take four times as long as equal ones and 0.14 ms more.
+    const uint64_t fewest = (uint64_t)((s.total_q + 127) / 128 > filled ? (s.total_q + 127) / 128 : filled) * s.n_h;
+    const uint64_t room = kScratch / ((uint64_t)s.total_q * s.n_h * (D + 2) * sizeof(float)), least = (uint64_t)s.total_q * s.n_h <= 2048 ? 256 : 512;
+    const uint64_t share = (fewest * keys + 2 * kNumCU - 1) / (2 * kNumCU), size = share > least ? share : least, most = room < kMostParts ? room : kMostParts;
+    const bool all = keys >= 2 * size, some = s.n_seq > 1 && s.total_k >= 4 * share + kWorth;
+    if (most < 2 || !(all || some)) {
         return over_tiles(tiles, s.n_h, [&](uint32_t left, uint32_t blocks) {
-            prompt_kernel<T, D, false><<<blocks, 256, 0, stream>>>(s, left, nullptr);
+            prompt_kernel<T, D, false><<<blocks, 256, 0, stream>>>(s, left, Cut{}, nullptr);
         });
     }
-    const hipError_t e = over_tiles(tiles, s.n_h, [&](uint32_t left, uint32_t blocks) {
-        prompt_kernel<T, D, true><<<dim3(blocks, (uint32_t)parts), 256, 0, stream>>>(s, left, scratch);
+    const Cut cut = {make_div32((uint32_t)size), (uint32_t)most, all ? (uint32_t)most : 1u};
+    // At least as many units as there are: one to a tile, and beyond those as many to a sequence's last tile as size goes into its keys, which
+    // is total_k / size for all sequences, and no more to each of the others, which are total_q / 128.
+    const uint64_t more = s.total_k / size, units = tiles + more + (all ? s.total_q / 128 * (more < most ? more : most - 1) : 0);
+    const hipError_t e = over_tiles((uint32_t)units, s.n_h, [&](uint32_t left, uint32_t blocks) {
+        prompt_kernel<T, D, true><<<blocks, 256, 0, stream>>>(s, left, cut, scratch);
     });
     if (e != hipSuccess) return e;
-    return over_tiles(tiles, s.n_h, [&](uint32_t left, uint32_t blocks) {
-        prompt_join_kernel<T, D><<<dim3(blocks, 128 * (D / 4) / 256), 256, 0, stream>>>(s, left, scratch, (uint32_t)parts);
-    });
+    prompt_join_kernel<T, D><<<s.total_q * ((s.n_h * (D / 4) + 255) / 256), 256, 0, stream>>>(s, cut, scratch);
+    return hipGetLastError();
 }
 
 }  // namespace
