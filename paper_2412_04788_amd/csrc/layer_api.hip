@@ -11,6 +11,11 @@ bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
 size_t elem_bytes(uint32_t type) { return type == GUIDE_F32 ? 4 : 2; }
 bool elem_aligned(const void *p, uint32_t type) { return (uintptr_t)p % elem_bytes(type) == 0; }
 
+// A stride between rows that there is only one of means nothing: it becomes the row's width.
+void one_row(uint64_t rows, int64_t &stride, uint64_t width) {
+    if (rows == 1) stride = (int64_t)width;
+}
+
 // A row-major typed tensor's pointer and row stride.
 int check_rows(guide_ctx *ctx, const char *name, const void *p, uint32_t type, int64_t stride, uint64_t width) {
     if (!p) return fail(ctx, GUIDE_E_ARG, "%s is NULL", name);
@@ -91,10 +96,13 @@ int check_cache(guide_ctx *ctx, const guide_cache *c) {
     return GUIDE_OK;
 }
 
-int cache_tokens(guide_ctx *ctx, const guide_cache *cache, const guide_cache_tokens *t, void *stream, bool read) {
+int cache_tokens(guide_ctx *ctx, const guide_cache *cache, const guide_cache_tokens *asked, void *stream, bool read) {
     if (!ctx) return GUIDE_E_ARG;
     GUIDE_TRY(check_cache(ctx, cache));
-    if (!t) return fail(ctx, GUIDE_E_ARG, "tokens is NULL");
+    if (!asked) return fail(ctx, GUIDE_E_ARG, "tokens is NULL");
+    guide_cache_tokens spec = *asked, *const t = &spec;
+    one_row(t->tokens, t->k_stride, cache->d);
+    one_row(t->tokens, t->v_stride, cache->d);
     GUIDE_TRY(check_16bit(ctx, t->type));
     if (t->tokens == 0) return GUIDE_OK;
     if (t->tokens > INT32_MAX) return fail(ctx, GUIDE_E_RANGE, "2^31 or more tokens");
@@ -111,9 +119,13 @@ int cache_tokens(guide_ctx *ctx, const guide_cache *cache, const guide_cache_tok
 
 extern "C" {
 
-int guide_quantise(guide_ctx *ctx, const guide_quantise_spec *s, void *stream) {
+int guide_quantise(guide_ctx *ctx, const guide_quantise_spec *asked, void *stream) {
     if (!ctx) return GUIDE_E_ARG;
-    if (!s) return fail(ctx, GUIDE_E_ARG, "spec is NULL");
+    if (!asked) return fail(ctx, GUIDE_E_ARG, "spec is NULL");
+    guide_quantise_spec spec = *asked, *const s = &spec;
+    one_row(s->rows, s->x_stride, s->cols);
+    one_row(s->rows, s->codes_stride, ((uint64_t)s->cols + 31) / 32 * s->bits * 4);
+    one_row(s->rows, s->scales_stride, ((uint64_t)s->cols + 31) / 32);
     GUIDE_TRY(check_quant(ctx, s->type, s->bits));
     if (s->rows == 0 || s->cols == 0) return GUIDE_OK;
     if (s->cols > INT32_MAX - 64) return fail(ctx, GUIDE_E_RANGE, "2^31 - 64 or more columns");
@@ -126,9 +138,15 @@ int guide_quantise(guide_ctx *ctx, const guide_quantise_spec *s, void *stream) {
     return launched(ctx, launch_quantise(*s, (hipStream_t)stream), "quantise launch");
 }
 
-int guide_rms_norm(guide_ctx *ctx, const guide_norm_spec *s, void *stream) {
+int guide_rms_norm(guide_ctx *ctx, const guide_norm_spec *asked, void *stream) {
     if (!ctx) return GUIDE_E_ARG;
-    if (!s) return fail(ctx, GUIDE_E_ARG, "spec is NULL");
+    if (!asked) return fail(ctx, GUIDE_E_ARG, "spec is NULL");
+    guide_norm_spec spec = *asked, *const s = &spec;
+    one_row(s->rows, s->x_stride, s->d);
+    one_row(s->rows, s->residual_stride, s->d);
+    one_row(s->rows, s->total_stride, s->d);
+    one_row(s->rows, s->codes_stride, ((uint64_t)s->d + 31) / 32 * s->bits * 4);
+    one_row(s->rows, s->scales_stride, ((uint64_t)s->d + 31) / 32);
     GUIDE_TRY(check_quant(ctx, s->type, s->bits));
     if (!(s->eps >= 0.0f) || !std::isfinite(s->eps)) return fail(ctx, GUIDE_E_ARG, "eps must be finite and not negative");
     if (s->d > GUIDE_NORM_MAX_WIDTH) return fail(ctx, GUIDE_E_RANGE, "width %u above %d", s->d, GUIDE_NORM_MAX_WIDTH);
@@ -145,9 +163,15 @@ int guide_rms_norm(guide_ctx *ctx, const guide_norm_spec *s, void *stream) {
     return launched(ctx, launch_norm(*s, (hipStream_t)stream), "norm launch");
 }
 
-int guide_product(guide_ctx *ctx, const guide_product_spec *s, void *stream) {
+int guide_product(guide_ctx *ctx, const guide_product_spec *asked, void *stream) {
     if (!ctx) return GUIDE_E_ARG;
-    if (!s) return fail(ctx, GUIDE_E_ARG, "spec is NULL");
+    if (!asked) return fail(ctx, GUIDE_E_ARG, "spec is NULL");
+    guide_product_spec spec = *asked, *const s = &spec;
+    one_row(s->m, s->a_codes_stride, (uint64_t)s->k / 32 * s->a_bits * 4);
+    one_row(s->m, s->a_scales_stride, s->k / 32);
+    one_row(s->n, s->w_codes_stride, s->k / 2);
+    one_row(s->n, s->w_scales_stride, s->k / 32);
+    one_row(s->m, s->out_stride, s->n);
     GUIDE_TRY(check_quant(ctx, s->type, s->a_bits));
     if (s->type == GUIDE_F32 && s->a_bits == 8)
         return fail(ctx, GUIDE_E_ARG, "8-bit activations into 32 bits: the matrix unit does not hold those sums to 32 bits");
@@ -167,9 +191,14 @@ int guide_product(guide_ctx *ctx, const guide_product_spec *s, void *stream) {
     return launched(ctx, launch_product(*s, ctx->layer_scratch, (hipStream_t)stream), "product launch");
 }
 
-int guide_prompt_attention(guide_ctx *ctx, const guide_prompt_spec *s, void *stream) {
+int guide_prompt_attention(guide_ctx *ctx, const guide_prompt_spec *asked, void *stream) {
     if (!ctx) return GUIDE_E_ARG;
-    if (!s) return fail(ctx, GUIDE_E_ARG, "spec is NULL");
+    if (!asked) return fail(ctx, GUIDE_E_ARG, "spec is NULL");
+    guide_prompt_spec spec = *asked, *const s = &spec;
+    one_row(s->total_q, s->q_stride, s->d);
+    one_row(s->total_q, s->out_stride, s->d);
+    one_row(s->total_k, s->k_stride, s->d);
+    one_row(s->total_k, s->v_stride, s->d);
     GUIDE_TRY(check_16bit(ctx, s->type));
     GUIDE_TRY(check_group_heads(ctx, s->n_h, s->n_kv, s->d));
     GUIDE_TRY(check_scale(ctx, s->scale));
@@ -201,11 +230,15 @@ size_t guide_cache_attention_workspace_bytes(uint32_t n_seq, uint32_t n_h, uint3
     return cache_attention_workspace(n_seq, n_h, n_kv, d, max_len);
 }
 
-int guide_cache_attention(guide_ctx *ctx, const guide_cache *cache, const guide_cache_queries *s, void *workspace, size_t workspace_bytes,
+int guide_cache_attention(guide_ctx *ctx, const guide_cache *cache, const guide_cache_queries *asked, void *workspace, size_t workspace_bytes,
                           void *stream) {
     if (!ctx) return GUIDE_E_ARG;
     GUIDE_TRY(check_cache(ctx, cache));
-    if (!s) return fail(ctx, GUIDE_E_ARG, "queries is NULL");
+    if (!asked) return fail(ctx, GUIDE_E_ARG, "queries is NULL");
+    guide_cache_queries spec = *asked, *const s = &spec;
+    one_row(s->n_seq, s->q_stride, cache->d);
+    one_row(s->n_seq, s->out_stride, cache->d);
+    one_row(s->n_seq, s->pages_stride, s->max_pages);
     GUIDE_TRY(check_16bit(ctx, s->type));
     GUIDE_TRY(check_group_heads(ctx, s->n_h, cache->n_kv, cache->d));
     GUIDE_TRY(check_scale(ctx, s->scale));

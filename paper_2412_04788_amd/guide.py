@@ -295,14 +295,7 @@ def _strided(t, dims: int, dtype=None):
         raise ValueError(f"a CUDA tensor of {dims} dimensions with a contiguous last one is needed")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"dtypes differ: {t.dtype} and {dtype}")
-    if dims > 1 and t.shape[0] == 1:                             # a stride of no meaning, which torch leaves as it comes
-        st = (_one_row(t), *st[1:])
     return t.data_ptr(), st
-
-
-def _one_row(t) -> int:
-    """A row stride that passes the library's checks, for a tensor of one row."""
-    return -(-t.shape[-1] // 16) * 16
 
 
 def _shaped(what: str, t, shape):
@@ -310,11 +303,9 @@ def _shaped(what: str, t, shape):
         raise ValueError(f"{what}: shape {tuple(t.shape)}, {tuple(shape)} is needed")
 
 
-def _counts(*n):
+def _too_many():
     """Counts go to the library in 32 bits."""
-    for x in n:
-        if x >> 32:
-            raise ValueError(f"{x} rows or tokens: fewer than 2^32 are needed")
+    return ValueError("2^32 or more rows, columns or tokens")
 
 
 def _codes(what: str, t, shape):
@@ -586,7 +577,8 @@ class Context:
         """Pointers and strides of code and scale buffers of `rows` rows of `cols` values."""
         if bits != 4 and bits != 8:
             raise ValueError(f"codes of {bits} bits: 4 or 8")
-        _counts(rows, cols)
+        if (rows | cols) >> 32:
+            raise _too_many()
         groups = -(-cols // MX_GROUP)
         return (*_codes("codes", codes, (rows, groups * 4 * bits)), *_codes("scales", scales, (rows, groups)))
 
@@ -629,7 +621,8 @@ class Context:
         """Causal attention of packed sequences: q, out [total_q, n_h, d], k, v [total_k, n_kv, d], starts int32 [n_seq + 1]."""
         shape, dtype = q.shape, q.dtype
         (tq, n_h, d), (tk, n_kv, dk), n = shape, k.shape, q_starts.numel()
-        _counts(tq, tk, n)
+        if (tq | tk | n) >> 32:
+            raise _too_many()
         _shaped("out", out, shape)
         _shaped("v", v, k.shape)
         _shaped("q_starts", q_starts, (n,))
@@ -653,7 +646,8 @@ class Context:
     def _cache_tokens(self, fn, k, v, slots, codes, scales, stream):
         cache = self._cache(codes, scales)
         shape = (slots.numel(), cache.n_kv, cache.d)
-        _counts(shape[0])
+        if shape[0] >> 32:
+            raise _too_many()
         _shaped("k", k, shape)
         _shaped("v", v, shape)
         (pk, ks), (pv, vs) = _strided(k, 3), _strided(v, 3, k.dtype)
@@ -677,7 +671,8 @@ class Context:
         cache = self._cache(codes, scales)
         shape = q.shape
         n_seq, n_h, d = shape
-        _counts(n_seq)
+        if n_seq >> 32:
+            raise _too_many()
         if d != cache.d:
             raise ValueError(f"head dimensions {d} and {cache.d}")
         _shaped("out", out, shape)
