@@ -29,8 +29,8 @@ CacheView view_of(const guide_cache &c) { return {c.codes, c.scales, c.n_pages, 
 
 // A lane handles eight channels of one token's keys and the same of its values (two loads on their way at a time), a quad of
 // lanes a group.  A block takes one KV head of 16 (d = 128) or 32 (d = 64) consecutive tokens: where their slots follow each
-// other, it writes two runs of codes and 16 or 32 bytes in a row of every scale row.  Bound by memory: 8192 tokens of 40 heads of
-// 128 (213 MB either way) are appended in 50 to 55 us and read back in 33.
+// other, it writes two runs of codes and 16 or 32 bytes in a row of every scale row.  8192 tokens of 40 heads of 128 (213 MB either way)
+// are read back in 33 us, at memory's rate (6.4 TB/s; a plain copy of as much 5.7 to 6.8), and appended in 50 to 55 (3.9 to 4.3).
 template <int T, int D, bool READ>
 __global__ __launch_bounds__(kBlock) void cache_tokens_kernel(CacheView c, guide_cache_tokens t) {
     using E = typename Elem<T>::type;
@@ -142,8 +142,8 @@ struct Piece {
 // become 16-bit values by conversions that apply the scale.  Values come a token to a word and are turned round in
 // registers: channel c of the lane's eight keys is its operand for row `col` of the c-th product.
 // The maximum that the exponentials are taken against moves only when a score exceeds it by more than 2^8.
-// Bound by memory: 64 sequences of 1000 to 16 000 tokens, 64 heads on 8 of 128, 87 us (381 MB, 4.4 TB/s) and 5.5 for the join; of
-// one sequence of 40 001 tokens (43.5 MB) 13 us, 4 of them until the first keys arrive.
+// 64 sequences of 1000 to 16 000 tokens, 64 heads on 8 of 128: 88 to 92 us (381 MB, 4.2 TB/s, where plain reads of as much reach 6.2)
+// and 5.5 for the join; of one sequence of 40 001 tokens (43.5 MB) 13 us, 4 of them until the first keys arrive.
 template <int T, int D>
 __global__ __launch_bounds__(kBlock, 3) void cache_attention_kernel(CacheView c, guide_cache_queries s, Div32 by_block, Split sp, void *ws) {
     using E = typename Elem<T>::type;

@@ -60,7 +60,7 @@ __device__ __forceinline__ void store4(typename Elem<T>::type *p, f32x4 v, uint3
 // A block takes 16 rows and 16 columns and its waves take turns along k, 512 at a time, straight from memory to registers: every code of
 // W is read once, by one wave, in runs of 64 bytes to a lane.  In step s of four, lane group g stands for group 4 g + s of
 // the 16, so a lane's four scale bytes are one word.  The waves' sums are joined in LDS, in the waves' order.
-// Bound by memory: one row against 28672 x 8192 27 us (125 MB, 4.6 TB/s).
+// Bound by memory, though not at its full rate: one row against 28672 x 8192 27 us (125 MB, 4.6 TB/s; plain reads of as much 6.6).
 template <int T, int ABITS, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void stream_kernel(guide_product_spec s) {
     using E = typename Elem<T>::type;
@@ -188,9 +188,9 @@ __device__ __forceinline__ Scales few_scales(const uint8_t *row, int groups) {
 // steps) at a time through registers.
 // Where there are too few tiles to fill the chip, k is split over blocks: split p sums split_groups groups (a multiple of
 // 16) and writes to row p m of `out`, which is then a plane of 32-bit sums for each split.
-// Large products are bound by the card's power as much as by the instructions: 8192 x 28672 x 8192 in 4 bits takes 880 to 950 us (4100
-// to 4350 TFLOP/s), 870 on the previous form with all codes zero where random ones took 1020, and the products alone, without loads and
-// reads, 810; 8 bits 1440 to 1510 us, products alone 1135.  Small ones are bound by the codes' way from memory.
+// Large products are bound by the card's power as much as by the instructions: 8192 x 28672 x 8192 in 4 bits takes 910 to 960 us (4000
+// to 4230 TFLOP/s), 870 on an earlier form with all codes zero where random ones took 1020, and the products alone, without loads and
+// reads, 810; 8 bits 1450 to 1520 us, products alone 1135.  Small ones are bound by the codes' way from memory.
 template <int T, int ABITS, int BM, int BN>
 __global__ __launch_bounds__(256) void tile_kernel(guide_product_spec s, uint32_t m_tiles, uint32_t n_tiles, uint32_t splits, uint32_t split_groups) {
     using E = typename Elem<T>::type;

@@ -324,7 +324,7 @@ struct Parts {
 
 // Four waves take 128 queries of one head, a wave 32 of them; the keys come in tiles of 64 through LDS, the next tile on its
 // way while one is worked on.  Two such blocks share a compute unit, so that one's exponentials run beside the other's products
-// (48 % of the matrix units' cycles in a pass of six prompts of 300 to 3900 tokens, 64 heads on 8 of 128: 440 us, 880 TFLOP/s of
+// (48 % of the matrix units' cycles in a pass of six prompts of 300 to 3900 tokens, 64 heads on 8 of 128: 434 us, 890 TFLOP/s of
 // visible pairs, and 3 % in vain in tiles that are partly masked; the waves of a block wait for its last one there).
 // SPLIT: a sequence of many keys gives every tile so many blocks, each of which takes its part of the keys that any of the queries sees,
 // and prompt_join_kernel joins the parts.
@@ -424,7 +424,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(guide_prompt_spec s, uin
 // multiplies -- the values of its last tile, the scores of its next --, the other takes exponentials, so that matrix and
 // vector units work side by side.  Both groups meet after every turn; group 1 is one turn behind.  Turn 2 t, of which group 0's
 // products are of tile t, sends for the keys of tile t + 1 and the values of tile t, which are needed from turn 2 t + 2 on.
-// 8192 queries over 32 768 keys, 32 heads on 8: 3110 to 3220 us, 1200 to 1240 TFLOP/s, 67 % of the matrix units' cycles; the
+// 8192 queries over 32 768 keys, 32 heads on 8: 3150 to 3310 us, 1160 to 1220 TFLOP/s, 65 % of the matrix units' cycles; the
 // group at its exponentials has more instructions to issue than the other's products leave room for.
 template <int T, int D>
 __global__ __launch_bounds__(512, 2) void prompt_pair_kernel(guide_prompt_spec s, uint32_t tiles) {
