@@ -21,29 +21,86 @@ struct Cut {
     }
 };
 
-// The sequence, the tile in it and the part of its keys that unit number `unit` of the packed queries is (sequences have
-// ceil(n_q / ROWS) tiles each, and without a cut a tile is a unit); false when there are fewer units.  Every lane of a wave looks
-// at one sequence at a time.
-struct Place { uint32_t q0, nq, k0, nk, tile, part, parts; };
-
 __device__ inline uint32_t clamped(int32_t v, uint32_t total) { return v < 0 ? 0u : (uint32_t)v > total ? total : (uint32_t)v; }
 
+// A lane's sequence.  Units of work: a tile of ceil(n_q / ROWS), or as many as a tile has parts.
 template <int ROWS, bool SPLIT>
-__device__ inline bool find_unit(const guide_prompt_spec &s, const Cut &cut, uint32_t unit, Place &p) {
+struct Sequence {
+    uint32_t q0 = 0, nq = 0, k0 = 0, nk = 0, parts = 1, units = 0;
+    __device__ Sequence(const guide_prompt_spec &s, const Cut &cut, uint32_t i) {
+        if (i >= s.n_seq) return;                                    // (all four starts in one trip to memory)
+        q0 = clamped(s.q_starts[i], s.total_q);
+        k0 = clamped(s.k_starts[i], s.total_k);
+        const uint32_t q1 = clamped(s.q_starts[i + 1], s.total_q), k1 = clamped(s.k_starts[i + 1], s.total_k);
+        nq = q1 > q0 ? q1 - q0 : 0, nk = k1 > k0 ? k1 - k0 : 0;
+        if (SPLIT && nq) parts = cut.parts(nq, nk);
+        units = (nq + ROWS - 1) / ROWS * parts;
+    }
+};
+
+// Units before every 64 sequences, for calls of so many of them that a walk over them in every block takes longer than this kernel does; the
+// last entry is the number of all.  Walked / by the table, a query over one key each, 8 heads of 64: 256 sequences 14.1 / 15.7 us, 512
+// 27.3 / 24.5, 4096 565 / 148; 2048 over 50 keys each, 32 heads of 128, 1572 / 703.
+constexpr uint32_t kMostSequences = 1u << 20, kWalked = 384, kTable = kMostSequences / 64 + 64;
+template <int ROWS, bool SPLIT>
+__global__ __launch_bounds__(1024) void prompt_table_kernel(guide_prompt_spec s, Cut cut, uint32_t *table) {
+    constexpr uint32_t kEach = kMostSequences / 64 / 1024;           // entries of a thread, one after the other
+    __shared__ uint32_t units[kMostSequences / 64], sums[16];
+    const uint32_t chunks = (s.n_seq + 63) / 64, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    for (uint32_t c = wave; c < chunks; c += 16) {
+        uint32_t sum = Sequence<ROWS, SPLIT>(s, cut, c * 64 + lane).units;
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) sum += __shfl_xor(sum, m);
+        if (lane == 0) units[c] = sum;
+    }
+    __syncthreads();
+    uint32_t mine[kEach], own = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; ++i) {
+        const uint32_t c = threadIdx.x * kEach + i;
+        mine[i] = own;
+        own += c < chunks ? units[c] : 0;
+    }
+    uint32_t upto = own;                                             // running sums over the threads
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const uint32_t o = __shfl_up(upto, m);
+        if (lane >= (uint32_t)m) upto += o;
+    }
+    if (lane == 63) sums[wave] = upto;
+    __syncthreads();
+    uint32_t before = upto - own;
+    for (uint32_t w = 0; w < wave; ++w) before += sums[w];
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; ++i) {
+        const uint32_t c = threadIdx.x * kEach + i;
+        if (c < chunks) table[c] = before + mine[i];
+    }
+    if (threadIdx.x == 1023) table[chunks] = before + own;
+}
+
+// The sequence, the tile in it and the part of its keys that unit number `unit` of the packed queries is; false when there are
+// fewer units.  Every lane of a wave looks at one sequence at a time.
+struct Place { uint32_t q0, nq, k0, nk, tile, part, parts; };
+
+template <int ROWS, bool SPLIT>
+__device__ inline bool find_unit(const guide_prompt_spec &s, const Cut &cut, const uint32_t *table, uint32_t unit, Place &p) {
     const uint32_t lane = threadIdx.x % 64;
-    uint32_t before = 0;
-    for (uint32_t s0 = 0; s0 < s.n_seq; s0 += 64) {
-        const uint32_t q = s0 + lane;
-        uint32_t a = 0, b = 0, k0 = 0, k1 = 0;                        // (keys too: one trip to memory for all four)
-        if (q < s.n_seq) {
-            a = clamped(s.q_starts[q], s.total_q);
-            b = clamped(s.q_starts[q + 1], s.total_q);
-            k0 = clamped(s.k_starts[q], s.total_k);
-            k1 = clamped(s.k_starts[q + 1], s.total_k);
+    uint32_t before = 0, s0 = 0;
+    if (table) {                                                     // the last 64 sequences that begin at the unit or before it
+        uint32_t end = (s.n_seq + 63) / 64;
+        if (unit >= table[end]) return false;
+        while (end - s0 > 1) {
+            const uint32_t mid = (s0 + end) / 2;
+            if (table[mid] <= unit) s0 = mid;
+            else end = mid;
         }
-        const uint32_t nk = k1 > k0 ? k1 - k0 : 0, parts = SPLIT && b > a ? cut.parts(b - a, nk) : 1;
-        const uint32_t units = b > a ? (b - a + ROWS - 1) / ROWS * parts : 0;
-        uint32_t sum = units;                                        // running sum over the lanes
+        before = table[s0];
+        s0 *= 64;
+    }
+    for (; s0 < s.n_seq; s0 += 64) {
+        const Sequence<ROWS, SPLIT> q(s, cut, s0 + lane);
+        uint32_t sum = q.units;                                      // running sum over the lanes
 #pragma unroll
         for (int m = 1; m < 64; m <<= 1) {
             const uint32_t o = __shfl_up(sum, m);
@@ -53,10 +110,10 @@ __device__ inline bool find_unit(const guide_prompt_spec &s, const Cut &cut, uin
         if (past) {
             const int w = __builtin_ctzll(past);
             auto of = [&](uint32_t x) __attribute__((always_inline)) { return (uint32_t)__builtin_amdgcn_readlane((int)x, w); };
-            p.q0 = of(a), p.nq = of(b) - p.q0, p.k0 = of(k0), p.nk = of(nk);
-            p.tile = unit - (before + of(sum - units)), p.part = 0, p.parts = 1;
+            p.q0 = of(q.q0), p.nq = of(q.nq), p.k0 = of(q.k0), p.nk = of(q.nk);
+            p.tile = unit - (before + of(sum - q.units)), p.part = 0, p.parts = 1;
             if constexpr (SPLIT) {
-                p.parts = of(parts);
+                p.parts = of(q.parts);
                 p.part = p.tile % p.parts, p.tile /= p.parts;
             }
             return true;
@@ -277,7 +334,7 @@ struct Rows {
 // Blocks go round the eight XCDs in turn: with a multiple of eight KV heads, the query heads of one KV head stay on one XCD, whose L2
 // then holds its keys once.
 template <int ROWS, bool SPLIT>
-__device__ __forceinline__ bool find_work(const guide_prompt_spec &s, const Cut &cut, uint32_t units, Place &p, uint32_t &head, uint32_t &kv) {
+__device__ __forceinline__ bool find_work(const guide_prompt_spec &s, const Cut &cut, const uint32_t *table, uint32_t units, Place &p, uint32_t &head, uint32_t &kv) {
     const uint32_t group = s.n_h / s.n_kv;
     uint32_t unit;
     if (s.n_kv % 8 == 0) {
@@ -289,7 +346,7 @@ __device__ __forceinline__ bool find_work(const guide_prompt_spec &s, const Cut 
         unit = blockIdx.x / s.n_h;
     }
     kv = head / group;
-    return find_unit<ROWS, SPLIT>(s, cut, units - 1 - unit, p);
+    return find_unit<ROWS, SPLIT>(s, cut, table, units - 1 - unit, p);
 }
 
 // Whether the wave's part of a staged tile of values, which it sent for itself, holds an infinity or a NaN.
@@ -329,7 +386,7 @@ struct Parts {
 // SPLIT: a sequence of many keys gives every tile so many blocks, each of which takes its part of the keys that any of the queries sees,
 // and prompt_join_kernel joins the parts.
 template <int T, int D, bool SPLIT>
-__global__ __launch_bounds__(256, 2) void prompt_kernel(guide_prompt_spec s, uint32_t units, Cut cut, float *scratch) {
+__global__ __launch_bounds__(256, 2) void prompt_kernel(guide_prompt_spec s, uint32_t units, Cut cut, const uint32_t *table, float *scratch) {
     using E = typename Elem<T>::type;
     constexpr int kRow = D * 2, kTileQ = 4 * kRowsPerWave;
     using SendK = Sender<D, true, 4>;
@@ -338,7 +395,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(guide_prompt_spec s, uin
     __shared__ uint32_t odd0[4], odd1[4];
     Place p;
     uint32_t head, kv;
-    if (!find_work<kTileQ, SPLIT>(s, cut, units, p, head, kv)) return;
+    if (!find_work<kTileQ, SPLIT>(s, cut, table, units, p, head, kv)) return;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int first = (int)(p.tile * kTileQ) + wave * kRowsPerWave, row = first + lane % 32;      // queries of the sequence
     const int nq = (int)p.nq, nk = (int)p.nk, shift = nk - nq;
@@ -427,7 +484,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(guide_prompt_spec s, uin
 // 8192 queries over 32 768 keys, 32 heads on 8: 3150 to 3310 us, 1160 to 1220 TFLOP/s, 65 % of the matrix units' cycles; the
 // group at its exponentials has more instructions to issue than the other's products leave room for.
 template <int T, int D>
-__global__ __launch_bounds__(512, 2) void prompt_pair_kernel(guide_prompt_spec s, uint32_t tiles) {
+__global__ __launch_bounds__(512, 2) void prompt_pair_kernel(guide_prompt_spec s, uint32_t tiles, const uint32_t *table) {
     using E = typename Elem<T>::type;
     constexpr int kRow = D * 2, kTileQ = 8 * kRowsPerWave;
     using SendK = Sender<D, true, 8>;
@@ -436,7 +493,7 @@ __global__ __launch_bounds__(512, 2) void prompt_pair_kernel(guide_prompt_spec s
     __shared__ uint32_t odd0[8], odd1[8];
     Place p;
     uint32_t head, kv;
-    if (!find_work<kTileQ, false>(s, Cut{}, tiles, p, head, kv)) return;
+    if (!find_work<kTileQ, false>(s, Cut{}, table, tiles, p, head, kv)) return;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int first = (int)(p.tile * kTileQ) + wave * kRowsPerWave, row = first + lane % 32;
     const int nq = (int)p.nq, nk = (int)p.nk, shift = nk - nq;
@@ -548,18 +605,16 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(guide_prompt_spec s, C
     constexpr uint32_t kHeads = 256 / (D / 4);
     const uint32_t groups = (s.n_h + kHeads - 1) / kHeads, query = blockIdx.x / groups;
     const uint32_t head = blockIdx.x % groups * kHeads + threadIdx.x / (D / 4), ch = threadIdx.x % (D / 4) * 4;
-    uint32_t count = 0;
-    for (uint32_t s0 = 0; s0 < s.n_seq && count == 0; s0 += 64) {
-        const uint32_t q = s0 + threadIdx.x % 64;
-        uint32_t a = 0, b = 0, nk = 0;
-        if (q < s.n_seq) {
-            a = clamped(s.q_starts[q], s.total_q);
-            b = clamped(s.q_starts[q + 1], s.total_q);
-            const uint32_t k0 = clamped(s.k_starts[q], s.total_k), k1 = clamped(s.k_starts[q + 1], s.total_k);
-            nk = k1 > k0 ? k1 - k0 : 0;
-        }
-        const uint64_t here = __ballot(a <= query && query < b);
-        if (here) count = (uint32_t)__builtin_amdgcn_readlane((int)cut.parts(b - a, nk), __builtin_ctzll(here));
+    uint32_t count = 0, s0 = 0;
+    for (uint32_t end = (s.n_seq + 63) / 64; s.n_seq > kWalked && end - s0 > 1;) {      // the last 64 sequences that begin at the query or before it
+        const uint32_t mid = (s0 + end) / 2;
+        if (clamped(s.q_starts[mid * 64], s.total_q) <= query) s0 = mid;
+        else end = mid;
+    }
+    for (s0 *= 64; s0 < s.n_seq && count == 0; s0 += 64) {
+        const Sequence<4 * kRowsPerWave, true> q(s, cut, s0 + threadIdx.x % 64);
+        const uint64_t here = __ballot(q.q0 <= query && query - q.q0 < q.nq);
+        if (here) count = (uint32_t)__builtin_amdgcn_readlane((int)q.parts, __builtin_ctzll(here));
     }
     if (count < 2 || head >= s.n_h) return;
     const Parts parts((float *)scratch, (uint64_t)s.total_q * s.n_h, cut.most);
@@ -606,6 +661,14 @@ hipError_t over_tiles(uint32_t tiles, uint32_t n_h, Launch launch) {
     return hipSuccess;
 }
 
+// The table for a call of many sequences (at the start of the scratch), or none.
+template <int ROWS, bool SPLIT>
+const uint32_t *make_table(const guide_prompt_spec &s, const Cut &cut, float *scratch, hipStream_t stream) {
+    if (s.n_seq <= kWalked) return nullptr;
+    prompt_table_kernel<ROWS, SPLIT><<<1, 1024, 0, stream>>>(s, cut, (uint32_t *)scratch);
+    return (const uint32_t *)scratch;
+}
+
 template <int T, int D>
 hipError_t prompt_as(const guide_prompt_spec &s, float *scratch, hipStream_t stream) {
     // The pairs of groups pay where their turns are many and their tiles of 256 queries fill the chip: 8192 queries over 32 768
@@ -615,8 +678,9 @@ hipError_t prompt_as(const guide_prompt_spec &s, float *scratch, hipStream_t str
     const uint64_t keys = (2ull * s.total_k > s.total_q ? 2ull * s.total_k - s.total_q : 0) / (2 * s.n_seq);     // that a query sees, about
     if constexpr (D == 128) {
         if (keys >= 4096 && (uint64_t)(s.total_q / 256) * s.n_h >= kNumCU) {
+            const uint32_t *table = make_table<256, false>(s, Cut{}, scratch, stream);
             return over_tiles(s.total_q / 256 + filled, s.n_h, [&](uint32_t left, uint32_t blocks) {
-                prompt_pair_kernel<T, D><<<blocks, 512, 0, stream>>>(s, left);
+                prompt_pair_kernel<T, D><<<blocks, 512, 0, stream>>>(s, left, table);
             });
         }
     }
@@ -630,23 +694,26 @@ hipError_t prompt_as(const guide_prompt_spec &s, float *scratch, hipStream_t str
     // 100.  Where they are equal after all, that is for nothing (16 over 4000 each 125 / 133, 64 over 1000 of 64 heads 232 / 244), so it
     // is done only where a sequence of all keys would take four times as long as equal ones and 0.14 ms more.
     const uint64_t fewest = (uint64_t)((s.total_q + 127) / 128 > filled ? (s.total_q + 127) / 128 : filled) * s.n_h;
-    const uint64_t room = kScratch / ((uint64_t)s.total_q * s.n_h * (D + 2) * sizeof(float)), least = (uint64_t)s.total_q * s.n_h <= 2048 ? 256 : 512;
+    const uint64_t room = (kScratch - kTable * sizeof(float)) / ((uint64_t)s.total_q * s.n_h * (D + 2) * sizeof(float)), least = (uint64_t)s.total_q * s.n_h <= 2048 ? 256 : 512;
     const uint64_t share = (fewest * keys + 2 * kNumCU - 1) / (2 * kNumCU), size = share > least ? share : least, most = room < kMostParts ? room : kMostParts;
     const bool all = keys >= 2 * size, some = s.n_seq > 1 && s.total_k >= 4 * share + kWorth;
     if (most < 2 || !(all || some)) {
+        const uint32_t *table = make_table<128, false>(s, Cut{}, scratch, stream);
         return over_tiles(tiles, s.n_h, [&](uint32_t left, uint32_t blocks) {
-            prompt_kernel<T, D, false><<<blocks, 256, 0, stream>>>(s, left, Cut{}, nullptr);
+            prompt_kernel<T, D, false><<<blocks, 256, 0, stream>>>(s, left, Cut{}, table, nullptr);
         });
     }
     const Cut cut = {make_div32((uint32_t)size), (uint32_t)most, all ? (uint32_t)most : 1u};
     // At least as many units as there are: one to a tile, and beyond those as many to a sequence's last tile as size goes into its keys, which
     // is total_k / size for all sequences, and no more to each of the others, which are total_q / 128.
     const uint64_t more = s.total_k / size, units = tiles + more + (all ? s.total_q / 128 * (more < most ? more : most - 1) : 0);
+    const uint32_t *table = make_table<128, true>(s, cut, scratch, stream);
+    float *const parts = scratch + kTable;
     const hipError_t e = over_tiles((uint32_t)units, s.n_h, [&](uint32_t left, uint32_t blocks) {
-        prompt_kernel<T, D, true><<<blocks, 256, 0, stream>>>(s, left, cut, scratch);
+        prompt_kernel<T, D, true><<<blocks, 256, 0, stream>>>(s, left, cut, table, parts);
     });
     if (e != hipSuccess) return e;
-    prompt_join_kernel<T, D><<<s.total_q * ((s.n_h * (D / 4) + 255) / 256), 256, 0, stream>>>(s, cut, scratch);
+    prompt_join_kernel<T, D><<<s.total_q * ((s.n_h * (D / 4) + 255) / 256), 256, 0, stream>>>(s, cut, parts);
     return hipGetLastError();
 }
 

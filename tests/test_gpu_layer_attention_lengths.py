@@ -15,7 +15,7 @@ def ctx():
 
 
 def _starts(torch, lengths):
-    return torch.tensor([sum(lengths[:i]) for i in range(len(lengths) + 1)], dtype=torch.int32, device="cuda")
+    return torch.cat((torch.zeros(1, dtype=torch.int64), torch.tensor(lengths).cumsum(0))).int().cuda()
 
 
 # queries and keys of every sequence: fewer blocks than the chip runs (all of them may be split) and more (those of up to 128
@@ -80,3 +80,32 @@ def test_a_long_sequence_among_short_ones_is_split(ctx):
         return min(times)
     # whole it takes as long as 60 000 / 4000 = 15 times one of those, in parts of a sixteenth as long as one
     assert best([100] * 15 + [60000]) < 4 * best([4000] * 16)
+
+
+MANY = {      # heads, KV heads, channels; queries and keys of every sequence; how many sequences to one that is checked
+    "short": (4, 2, 64, [i % 6 for i in range(3000)], [(i * 7) % 11 for i in range(3000)], 1),
+    "empty_ones_around": (8, 8, 128, [0] * 1000 + [2, 0, 150] * 3 + [0] * 1000, [1] * 1000 + [3, 5, 400] * 3 + [0] * 1000, 1),
+    "one_long": (32, 8, 128, [1] * 500, [3] * 440 + [40000] + [5] * 59, 1),
+    "few_queries": (2, 1, 64, [0] * 500 + [2, 130], [9] * 500 + [9000, 7000], 1),
+    "long_ones": (64, 1, 128, [3] * 400, [4100 + i for i in range(400)], 37),
+}
+
+
+@pytest.mark.parametrize("case", MANY)
+def test_many_sequences(ctx, case):
+    """Hundreds to thousands of sequences, which blocks find by a table."""
+    import torch
+    heads, kv, d, q_len, k_len, every = MANY[case]
+    gen = torch.Generator("cuda").manual_seed(7)
+    q, k, v = (torch.randn(n, h, d, generator=gen, device="cuda").bfloat16() for n, h in ((sum(q_len), heads), (sum(k_len), kv), (sum(k_len), kv)))
+    out = torch.full_like(q, math.nan)
+    ctx.prompt_attention(q, k, v, _starts(torch, q_len), _starts(torch, k_len), out)
+    assert not out.isnan().any()
+    a = b = 0
+    for i, (nq, nk) in enumerate(zip(q_len, k_len)):
+        if nq and i % every == 0:
+            sees = torch.arange(nk, device="cuda")[None] <= torch.arange(nq, device="cuda")[:, None] + nk - nq
+            want, size = ref.attention(q[a:a + nq], k[b:b + nk], v[b:b + nk], sees, d ** -0.5)
+            err, bound = (out[a:a + nq].double() - want).abs(), ref.attention_bound(want, size, v[b:b + nk], nk, torch.bfloat16)
+            assert bool((err <= bound).all()), (i, nq, nk, float((err / bound).max()))
+        a, b = a + nq, b + nk

@@ -131,3 +131,16 @@ def test_counts_that_32_bits_do_not_hold(ctx):
                  lambda: ctx.cache_attention(many, *cache, starts[:1].expand(n, 1), starts[:1].expand(n), many)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_as_many_sequences_as_there_may_be(ctx):
+    """2^20 sequences of one token each: their blocks find them in much less time than a walk over them takes (minutes)."""
+    import torch
+    n, heads, d = 1 << 20, 8, 64
+    gen = torch.Generator("cuda").manual_seed(5)
+    k, v = (torch.randn(n, 1, d, generator=gen, device="cuda").bfloat16() for _ in range(2))
+    q = torch.ones(1, heads, d, dtype=torch.bfloat16, device="cuda").expand(n, heads, d).contiguous()
+    out = torch.full_like(q, math.nan)
+    starts = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    ctx.prompt_attention(q, k, v, starts, starts, out)
+    assert torch.equal(out, v.expand(n, heads, d))
